@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * WL * WR) void middle_kernel(MiddleArgs a, Epil
     for (int q = 0; q < STAGES; ++q) load(q);
     int stage = 0;
     for (int t = t0; t < t1; ++t) {
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 1) * LOADS) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 1) * LOADS) : "memory");
         const uint16_t* const x_lds = product_tiles + stage * (STAGE / 2);
         const float* const w_lds = reinterpret_cast<const float*>(x_lds + 3 * L);
 #pragma unroll
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * WL * WR) void middle_kernel(MiddleArgs a, Epil
         load(stage);
         stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     static_assert(!Epilogue::TURNS || BL * BR * 2 <= STAGES * STAGE, "the wavefronts' values fit");
     epi.template finish<NL, NR>(acc, tl * BL + wl * (BL / WL), tr * BR + wr * (BR / WR), tr * WR + wr, split, lane, product_tiles + wave * (NL * 16 * NR * 16));
 }

@@ -220,7 +220,7 @@ __device__ __forceinline__ void product(const ProductArgs& a, const Epilogue& ep
         for (int i = 0; i < LOADS; ++i) load(i);
         loaded();
     }
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 1) * LOADS) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 1) * LOADS) : "memory");
 #pragma unroll
     for (int i = 0; i < NL; ++i) read_l(i, 0, 0);
 #pragma unroll

@@ -309,7 +309,8 @@ __global__ __launch_bounds__(512) void sweep_kernel(SweepArgs a) {
 #pragma unroll
     for (int k = 0; k < STAGES - 1; ++k) bring(t0 + k, into++);
     for (int step = t0; step < t1; ++step) {
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 2) * LOADS) : "memory");
+        // (lgkmcnt: what is brought now goes to the place that the step before was read from)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * LOADS) : "memory");
         bring(step + STAGES - 1, into);
         into = into + 1 == STAGES ? 0 : into + 1;
         const uint16_t* const tile = product_tiles + stage * STAGE;
