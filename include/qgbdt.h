@@ -356,7 +356,7 @@ QGBDT_API int qgbdt_softmax_loss(qgbdt_ctx* ctx, const void* x, const void* weig
 /* Gradients of sum_i row_weight[i] * loss[i] (row_weight: the gradient that arrives at each row's loss, dev float[n]):
  * with D[i][j] = row_weight[i] * (exp(x[i].weight[j] - lse[i]) - [j = target[i]]), grad_x = D weight, grad_weight = D^T x.  `lse` as
  * qgbdt_softmax_loss gives it for the same x and weight.  Rows without a target or with a row_weight of 0 add nothing,
- * whatever x and lse hold there.  grad_x: dev [n][dim] or NULL; grad_weight: dev [n_classes][dim] or NULL. */
+ * whatever x and lse hold there and also where a class has infinite weights (which make the columns of grad_x that they stand in NaN).  grad_x: dev [n][dim] or NULL; grad_weight: dev [n_classes][dim] or NULL. */
 QGBDT_API int qgbdt_softmax_gradients_bytes(int64_t n, int32_t dim, int64_t n_classes, int32_t dtype, int64_t x_stride, int64_t weight_stride,
                                   size_t* bytes);
 QGBDT_API int qgbdt_softmax_gradients(qgbdt_ctx* ctx, const void* x, const void* weight, int32_t dtype, int64_t n, int32_t dim, int64_t n_classes,

@@ -92,12 +92,12 @@ __global__ __launch_bounds__(256) void few_scores_kernel(FewArgs a) {
     const int64_t blocks = (a.n_classes + 15) / 16, waves = (int64_t)gridDim.x * 4;
     const uint16_t* const xr = a.x + (int64_t)(s < a.n ? s : a.n - 1) * a.x_ld;
     const int dp = (a.dim + 7) / 8 * 8;
-    float u = 0.0f, b = 0.0f, f = 0.0f;
+    float u = 0.0f, b = 0.0f;
     int64_t t = -1;
     if (GRAD && s < a.n) {
         t = target_of(a.target, a.target_bytes, s, a.n_classes);
         if (t >= 0) u = a.weight[s] / *a.common;
-        if (u != 0.0f) { f = LOG2E; b = -a.lse[s] * LOG2E; }
+        if (u != 0.0f) b = -a.lse[s] * LOG2E;
     }
     float top = -__builtin_inff(), sum = 0.0f;
     for (int64_t block = a.parts > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave; block < blocks; block += a.parts > 1 ? (int64_t)gridDim.x : waves) {
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void few_scores_kernel(FewArgs a) {
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                v[e] = u * __builtin_amdgcn_exp2f(fmaf(acc[e], f, b));
+                v[e] = u != 0.0f ? u * __builtin_amdgcn_exp2f(fmaf(acc[e], LOG2E, b)) : 0.0f;  // (left out: whatever the score is)
                 if (first + e == t) v[e] -= u;
             }
             if (s < a.n) {

@@ -236,23 +236,26 @@ struct GradEpilogue {
         const float unit = *common;
         const bool whole = col0 + CW <= cols;
         if (PIECES > 1 && back_l) scale_back(acc, back_l, back_r, row0, col0, rows, cols, lane);
+        // Rows that are left out, bit i: zeros, chosen when the values are packed and not multiplied, since their x of zeros makes scores that are no
+        // numbers with infinite weights.
+        uint32_t left = 0;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int row = row0 + i * 16 + (lane & 15);
-            // (of a row that is left out the scores are not looked at: exp2(0 s + 0) times 0; its x has been made zeros)
-            float u = 0.0f, f = 0.0f, b = 0.0f;
+            float u = 0.0f, b = 0.0f;
             int64_t t = -1;
             if (row < rows) {
                 t = target_of(target, target_bytes, row, n_classes);
                 if (t >= 0) u = weight[row] / unit;
-                if (u != 0.0f) { f = LOG2E; b = -lse[row] * LOG2E; }
+                if (u != 0.0f) b = -lse[row] * LOG2E;
             }
             const int64_t at = t - first - col0 - h4;
             const int want = t >= 0 && at >= 0 && at < CW ? (int)at : -1;
 #pragma unroll
             for (int j = 0; j < NR; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = u * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], f, b));
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = u * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, b));
+            left |= (u == 0.0f ? 1u : 0u) << i;
             if (__ballot(want >= 0) != 0)
 #pragma unroll
                 for (int j = 0; j < NR; ++j)
@@ -266,6 +269,7 @@ struct GradEpilogue {
                     for (int e = 0; e < 4; ++e)
                         if (col0 + j * 16 + h4 + e >= cols) acc[i][j][e] = 0.0f;
         }
+        const bool any_left = __ballot(left != 0) != 0;
 #pragma unroll 1
         for (int s = 0; s < PIECES; ++s) {
             // (16 consecutive rows put the same piece into 16 different places of 256 bytes)
@@ -280,6 +284,7 @@ struct GradEpilogue {
                         o.h[e] = to_bf16(acc[i][j][e]);
                         if (PIECES > 1) acc[i][j][e] -= from_bf16(o.h[e]);
                     }
+                    if (any_left) { o.v.x = left >> i & 1 ? 0u : o.v.x; o.v.y = left >> i & 1 ? 0u : o.v.y; }
                     *reinterpret_cast<uint2*>(own + r * CW + ((j * 2 + (lane >> 5)) ^ turn) * 8 + (h4 & 4)) = o.v;
                 }
             }

@@ -99,6 +99,20 @@ __global__ __launch_bounds__(512) void sweep_kernel(SweepArgs a) {
                 x[i][k][q] = __builtin_bit_cast(bf16x8, v);
             }
     }
+    // Whether a class that is kept has weights that are not finite: only then is a score of a row that is left out, and so all zeros, no zero.
+    bool odd = false;
+    if constexpr (MODE == SWEEP_CLASSES) {
+        constexpr uint32_t EXPONENT = SP::F16 ? 0x7c007c00u : 0x7f807f80u, ONE = SP::F16 ? 0x04000400u : 0x00800080u;
+        uint32_t over = 0;  // exponents of ones run over into the sign's place
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                const uint4 v = __builtin_bit_cast(uint4, x[i][k][0]);
+                over |= ((v.x & EXPONENT) + ONE) | ((v.y & EXPONENT) + ONE) | ((v.z & EXPONENT) + ONE) | ((v.w & EXPONENT) + ONE);
+            }
+        odd = __ballot((over & 0x80008000u) != 0) != 0;
+    }
     float b[2], u[2];
     int t[2];
     if constexpr (MODE == SWEEP_ROWS) {
@@ -264,6 +278,17 @@ __global__ __launch_bounds__(512) void sweep_kernel(SweepArgs a) {
                         acc[i][j][e] = v;
                     }
                 }
+            if (odd) {
+                asm volatile("" ::: "memory");  // (the weights are read again, not kept)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool left_out = terms[j * 16 + g * 4 + e].u == 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) acc[i][j][e] = left_out ? 0.0f : acc[i][j][e];
+                    }
+            }
         }
         // its k-th value is that of swept row 16 (k / 4 % 2) + 4 (k / 8) + k % 4, and so are the other operand's
         if constexpr (MODE != SWEEP_STATS)
@@ -340,11 +365,14 @@ __global__ __launch_bounds__(512) void sweep_kernel(SweepArgs a) {
         } else {
             if (row >= a.n_kept) continue;
             const float by = (MODE == SWEEP_ROWS ? u[i] : 1.0f) * (a.slab ? 1.0f : *a.unit);
+            const bool left_out = MODE == SWEEP_ROWS && u[i] == 0.0f;  // (zeros, whatever its sums are)
 #pragma unroll
             for (int m = 0; m < NM; ++m) {
                 const int col = m * 16 + g * 4;
                 if (col >= a.dim) continue;
-                const float v[4] = {out[i][m][0] * by, out[i][m][1] * by, out[i][m][2] * by, out[i][m][3] * by};
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = left_out ? 0.0f : out[i][m][e] * by;
                 if (a.slab) {
                     *reinterpret_cast<float4*>(a.slab + split * a.slab_size + row * a.slab_ld + col) = make_float4(v[0], v[1], v[2], v[3]);
                 } else {
