@@ -12,27 +12,6 @@
 
 namespace qgbdt {
 
-// The common weight: the first one that counts.  Whatever it is, D in units of it times it is what is wanted; where all are the same, as
-// for a mean, D keeps p - 1 and p without a second rounding.  For a whole workgroup; 1 where none counts.
-__device__ __forceinline__ float common_weight(const void* target, int target_bytes, int64_t rows, int64_t n_classes, const float* __restrict__ weight) {
-    __shared__ unsigned int found;
-    __shared__ float value;
-    if (threadIdx.x == 0) value = 1.0f;
-    for (int64_t at = 0; at < rows; at += 256) {
-        __syncthreads();
-        if (threadIdx.x == 0) found = 256;
-        __syncthreads();
-        const int64_t i = at + threadIdx.x;
-        const float u = i < rows ? weight[i] : 0.0f;
-        if (fabsf(u) > 1e-30f && fabsf(u) < 1e30f && target_of(target, target_bytes, i, n_classes) >= 0) atomicMin(&found, threadIdx.x);
-        __syncthreads();
-        if (found == threadIdx.x) value = u;
-        if (found < 256) break;
-    }
-    __syncthreads();
-    return value;
-}
-
 // What rows are left out by, and what the gradients need of them; all null or zero: no row is left out.
 struct LeftOut {
     const void* target;
@@ -40,6 +19,8 @@ struct LeftOut {
     int64_t n_classes;
     const float* weight;
     const float* lse;
+    const uint32_t* tops;  // not null: of weight_kernel
+    int n_tops;
     float* common;      // not null: written
     RowTerms* terms;    // not null: written, up to a multiple of SWEEP_TILE with rows that are left out
     __device__ __forceinline__ bool live(int64_t row) const { return !target || (target_of(target, target_bytes, row, n_classes) >= 0 && weight[row] != 0.0f); }
@@ -47,7 +28,54 @@ struct LeftOut {
         if (row < rows && live(row)) return {-lse[row] * LOG2E, weight[row] / unit, (int)target_of(target, target_bytes, row, n_classes), back};
         return {-__builtin_inff(), 0.0f, -1, back};
     }
+    // bits of a row's weight without its sign, 0 where it does not count or is not finite
+    __device__ __forceinline__ uint32_t size_of_weight(int64_t row) const {
+        const int64_t t = target_of(target, target_bytes, row, n_classes);  // (both are requested at once)
+        const uint32_t b = __float_as_uint(weight[row]) & 0x7fffffffu;
+        return t >= 0 && b < 0x7f800000u ? b : 0u;
+    }
 };
+
+__device__ __forceinline__ uint32_t largest_of_workgroup(uint32_t v) {
+    __shared__ uint32_t part[4];
+    for (int o = 32; o > 0; o >>= 1) { const uint32_t b = __shfl_xor(v, o); v = b > v ? b : v; }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    const uint32_t a = part[0] > part[1] ? part[0] : part[1], b = part[2] > part[3] ? part[2] : part[3];
+    return a > b ? a : b;
+}
+
+// The common weight: the largest finite one among the rows that count, 1 where none does.  D in units of it is at most 1 in size, and where all
+// weights are the same, as for a mean, D keeps p - 1 and p without a second rounding.  For a whole workgroup, from all rows where they are
+// few, else from the maxima of weight_kernel: every workgroup that lays rows out needs it, wherever the rows that count begin.
+constexpr int64_t WEIGHTS_AT_ONCE = 2048;  // (gradients of 2000 x 250 bf16 against 20,000 classes: 313 us, with the launch 319)
+constexpr int WEIGHT_BLOCKS = 256;
+__device__ __forceinline__ float common_weight(const LeftOut& src, int64_t rows) {
+    uint32_t top = 0;
+    if (src.tops) {
+        if ((int)threadIdx.x < src.n_tops) top = src.tops[threadIdx.x];
+    } else {
+#pragma unroll
+        for (int k = 0; k < (int)(WEIGHTS_AT_ONCE / 256); ++k) {
+            const int64_t i = threadIdx.x + k * 256;
+            const uint32_t b = i < rows ? src.size_of_weight(i) : 0u;
+            top = b > top ? b : top;
+        }
+    }
+    top = largest_of_workgroup(top);
+    return top ? __uint_as_float(top) : 1.0f;
+}
+
+// Up to WEIGHT_BLOCKS maxima of the rows' weights.  Bound by latency, with very many rows by memory (100,003 rows: 3 us).
+__global__ __launch_bounds__(256) void weight_kernel(LeftOut src, int64_t rows, uint32_t* __restrict__ tops) {
+    uint32_t top = 0;
+    const int64_t step = (int64_t)gridDim.x * 256;
+#pragma unroll 4
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows; i += step) { const uint32_t b = src.size_of_weight(i); top = b > top ? b : top; }
+    top = largest_of_workgroup(top);
+    if (threadIdx.x == 0) tops[blockIdx.x] = top;
+}
 
 // A matrix as the products read it: rows of `dp` elements (a multiple of 8, zeros behind the row's end), fp32 values in three
 // pieces.  Rows that are left out become zeros, whatever they hold.  Bound by memory (8192 x 2048 bf16: 14 us, 4.8 TB/s).
@@ -56,7 +84,7 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const typename E::T* __res
                                                       uint16_t* __restrict__ out, int64_t piece, LeftOut src) {
     const int64_t t0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
     if (src.terms || (src.common && blockIdx.x == 0)) {
-        const float unit = common_weight(src.target, src.target_bytes, rows, src.n_classes, src.weight);
+        const float unit = common_weight(src, rows);
         if (t0 == 0) *src.common = unit;
         if (src.terms)
             for (int64_t i = t0; i < (rows + SWEEP_TILE - 1) / SWEEP_TILE * SWEEP_TILE; i += step) src.terms[i] = src.of(i, rows, unit, 1.0f);
@@ -99,7 +127,7 @@ __global__ __launch_bounds__(256) void lay_out_fp32_kernel(const float* __restri
     const int64_t step = (int64_t)gridDim.x * per;
     float unit = 1.0f;
     if (src.terms || (src.common && blockIdx.x == 0)) {
-        unit = common_weight(src.target, src.target_bytes, rows, src.n_classes, src.weight);
+        unit = common_weight(src, rows);
         if (blockIdx.x == 0 && threadIdx.x == 0) *src.common = unit;
     }
     const int64_t filled = src.terms ? (rows + SWEEP_TILE - 1) / SWEEP_TILE * SWEEP_TILE : rows;
@@ -645,7 +673,7 @@ struct SoftmaxPlan {
     bool x_slabs, w_slabs;
     int64_t ld_d, slab_ld;
     // offsets in the scratch block
-    size_t common, terms, x16, w16, x_back, w_back, x, w, part, d, xs, ws, bytes;
+    size_t common, tops, terms, x16, w16, x_back, w_back, x, w, part, d, xs, ws, bytes;
 };
 
 static SoftmaxPlan make_softmax_plan(int64_t n, int dim, int64_t n_classes, int dtype, int64_t x_stride, int64_t w_stride, bool gradients) {
@@ -686,6 +714,8 @@ static SoftmaxPlan make_softmax_plan(int64_t n, int dim, int64_t n_classes, int 
         return p;
     }
     p.slab_ld = (dim + 3) / 4 * 4;
+    p.common = take(4);
+    p.tops = take(WEIGHT_BLOCKS * 4);
     if (p.few) {
         const int pieces = (dim + 3) / 4;
         p.lanes = 1;
@@ -697,7 +727,6 @@ static SoftmaxPlan make_softmax_plan(int64_t n, int dim, int64_t n_classes, int 
         if (p.each < least) p.each = least;
         p.strips = (n_classes + p.each - 1) / p.each;
         p.ld_d = (n_classes + 15) / 16 * 16;
-        p.common = take(4);
         p.x = take((size_t)n * p.dp * 2 * p.pieces);
         p.d = take((size_t)n * p.ld_d * 4);
         p.xs = take((size_t)p.strips * n * p.slab_ld * 4);
@@ -710,7 +739,6 @@ static SoftmaxPlan make_softmax_plan(int64_t n, int dim, int64_t n_classes, int 
         p.w_splits = sweep_splits(n_classes, n, dtype, sweep_parts(n_classes, dim), true);
         p.x_slabs = p.x_splits > 1;
         p.w_slabs = p.w_splits > 1;
-        p.common = take(4);
         if (halves) {
             p.x16 = take((size_t)n * p.dp * 4);
             p.x_back = take((size_t)n * 4);
@@ -739,7 +767,6 @@ static SoftmaxPlan make_softmax_plan(int64_t n, int dim, int64_t n_classes, int 
     if (p.middle) p.x_splits = middle_splits(n, dim, p.strip / PK);
     p.x_slabs = p.x_splits > 1 || p.strips > 1;
     p.w_slabs = p.w_splits > 1 || p.row_blocks > 1;
-    p.common = take(4);
     if (halves) {
         p.x16 = take((size_t)p.row_block * p.dp * 4);
         p.x_back = take((size_t)p.row_block * 4);
@@ -883,8 +910,11 @@ static void gradients(qgbdt_ctx* ctx, const SoftmaxPlan& p, const typename E::T*
     const uint16_t* const xp = reinterpret_cast<const uint16_t*>(s + p.x);
     const uint16_t *const x16 = reinterpret_cast<const uint16_t*>(s + p.x16), *const w16 = reinterpret_cast<const uint16_t*>(s + p.w16);
     const float *const x_back = reinterpret_cast<const float*>(s + p.x_back), *const w_back = reinterpret_cast<const float*>(s + p.w_back);
+    uint32_t* const tops = n > WEIGHTS_AT_ONCE ? reinterpret_cast<uint32_t*>(s + p.tops) : nullptr;
+    const int n_tops = (int)(n < WEIGHT_BLOCKS * 1024 ? (n + 1023) / 1024 : WEIGHT_BLOCKS);
+    if (tops) hipLaunchKernelGGL(weight_kernel, dim3(n_tops), dim3(256), 0, ctx->stream, LeftOut{target, target_bytes, n_classes, weight, lse, nullptr, 0, nullptr, nullptr}, n, tops);
     auto lay_out_x = [&](int64_t r0, int64_t rows, float* common, RowTerms* terms) {
-        const LeftOut src = {static_cast<const char*>(target) + r0 * target_bytes, target_bytes, n_classes, weight + r0, lse + r0, common, terms};
+        const LeftOut src = {static_cast<const char*>(target) + r0 * target_bytes, target_bytes, n_classes, weight + r0, lse + r0, tops, n_tops, common, terms};
         if (halves) lay_out_fp32(ctx, p, x + r0 * x_stride, x_stride, rows, dim, s + p.x16, s + p.x, s + p.x_back, src);
         else lay_out(ctx, p, x + r0 * x_stride, x_stride, rows, dim, s + p.x, src);
     };
