@@ -343,9 +343,11 @@ QGBDT_API int qgbdt_embed_gradient(qgbdt_ctx* ctx, const void* tokens, int32_t t
  * lse[i] = log sum_j exp(x[i].weight[j]), loss[i] = lse[i] - x[i].weight[target[i]]; targets outside 0 .. n_classes-1
  * leave the row out: loss 0.  A score that is NaN or +infinity makes its row's lse NaN, one of -infinity adds nothing; an infinite value of
  * QGBDT_F32, whose values go into the products in pieces, makes its scores NaN.  x: dev [n] rows of dim, x_stride apart; weight: dev [n_classes]
- * rows of dim, weight_stride apart; target: dev [n]; loss, lse: dev float[n].  dtype QGBDT_F32 (scores to fp32 accuracy) or
- * _BF16 (exact products, sums in fp32); not _F16, in which the probabilities of many classes vanish.  x and weight are 16-byte aligned
- * when dtype is _BF16 and dim and their stride are multiples of 8 (else any alignment; the call then reads them
+ * rows of dim, weight_stride apart; target: dev [n]; loss, lse: dev float[n].  dtype QGBDT_F32 or _BF16 (exact products, sums in fp32); not _F16, in
+ * which the probabilities of many classes vanish.  The products of QGBDT_F32, of values between 2^-100 and 2^120 in size, are off by 20 units of 2^-24 of their
+ * magnitudes' sum at most, whatever the rows' own range is, and are added up in fp32.  They are made of two pieces per value where that holds of
+ * them and of three where it does not, which a call sees from all its rows and classes: the others' values can change a score by so much.  x and weight are
+ * 16-byte aligned when dtype is _BF16 and dim and their stride are multiples of 8 (else any alignment; the call then reads them
  * through a copy in the scratch block).  n < 2^31, n_classes <= 2^27, dim <= 65536. */
 QGBDT_API int qgbdt_softmax_loss_bytes(int64_t n, int32_t dim, int64_t n_classes, int32_t dtype, int64_t x_stride, int64_t weight_stride,
                              size_t* bytes);

@@ -45,11 +45,20 @@ struct ProductArgs {
 //  * Three of bfloat16, hi + mid + lo (8 bits each, to the nearest): any value, and the six products whose size is at least 2^-18 of the largest,
 //    smallest first.  What is left out is below 2^-26 of |l||r|, less than fp32's own rounding.
 //  * Two of fp16, hi + lo (11 bits each), of rows scaled by a power of two that brings their largest value to 2^14 .. 2^15: half the
-//    products.  Values down to 2^-16 of their row's largest keep 22 bits, smaller ones what lies above 2^-39 of it; what is left out, lo lo, is
-//    below 2^-24 of |l||r|.  For scores, whose error counts against the length of the rows; D, whose small values count for
-//    themselves where a class is rare, is held in bfloat16 pieces.
+//    products.  Values down to 2^-17 of their row's largest keep 22 bits, smaller ones what lies above 2^-39 of it; what is left out, lo lo, is
+//    below 2^-22 of |l||r|.  For scores, where the rows allow it (in_three_pieces).
 // Nibble s of these: the piece of segment s.
 constexpr uint32_t SIX_L = 0x001012, SIX_R = 0x010210, THREE_L = 0x001, THREE_R = 0x010;
+
+// What rows of fp32 values say about two pieces of fp16, found when they are laid out.  A value below 2^-17 of its row's largest, a FAINT one, is off by
+// up to 2^-39 of that.  Without such a value in any row a score is off by 3 2^-22 of the sum of its terms' magnitudes at most.  With them it depends on
+// what they meet: a LOOSE row has more than a quarter of its values below 2^-9 of its largest, zeros among them.  Where no row of either matrix is
+// loose, any two have half of their `dim` values above that in common, so the magnitudes add up to dim / 2 * 2^-18 * |largest l||largest r| at
+// least, and the faint ones, a quarter of each row at most, add an error of dim / 2 * 2^-39 of the same: 2^-21.  Together 20 units of fp32.
+// WIDE: a row's largest value is beyond 2^-50 .. 2^50, and scaling the scores back could leave fp32's range on the way.
+// Scores are of three bfloat16 pieces where that does not hold, of two fp16 ones where it does.
+enum { RANGE_LOOSE = 1, RANGE_FAINT = 2, RANGE_WIDE = 4 };
+__device__ __forceinline__ bool in_three_pieces(uint32_t range) { return (range & RANGE_WIDE) || (range & (RANGE_LOOSE | RANGE_FAINT)) == (RANGE_LOOSE | RANGE_FAINT); }
 
 // A read of 16 bytes per lane takes 16 lanes at a time from 64 banks, so 16 consecutive rows (128 bytes each) have to put the same piece
 // into 16 different places of 256 bytes: piece c of row r lies at c ^ (r / 2) % 8.
@@ -153,22 +162,31 @@ __host__ __device__ constexpr int product_lds(int bl, int br, int threads, int s
 // the loads have STAGES - 1 steps to arrive.  Operands of r are read again into the registers of those just used.
 // A lane has C[l][r] of l = lane % 16 and r = 4 (lane / 16) + 0..3 of each block of 16 x 16: what is summed or stored along r lies in
 // few lanes.
-template <int BL, int BR, int WL, int WR, int STAGES, bool F16, bool LT, bool RT, class Epilogue>
-__device__ __forceinline__ void product(const ProductArgs& a, const Epilogue& epi, int block) {
+struct ProductPlace {
+    int tl, tr, split;  // tile of l and of r, part of k
+};
+// Neighbouring tiles on one XCD: workgroups go to the XCDs in turn, so XCD x takes the x-th eighth of the tiles, in
+// bands of 8 tiles of l, along r.  False: a workgroup without a tile.
+__device__ __forceinline__ bool product_place(const ProductArgs& a, int block, ProductPlace& p) {
+    const int total = a.tiles_l * a.tiles_r * a.splits, per = (total + 7) >> 3;
+    const int id = (block & 7) * per + (block >> 3);
+    if ((block >> 3) >= per || id >= total) return false;
+    const int per_split = a.tiles_l * a.tiles_r, in = id % per_split;
+    p.split = id / per_split;
+    const int band = in / (8 * a.tiles_r), left = a.tiles_l - band * 8, height = left < 8 ? left : 8;
+    const int inb = in - band * 8 * a.tiles_r;
+    p.tl = band * 8 + inb % height;
+    p.tr = inb / height;
+    return true;
+}
+
+template <int BL, int BR, int WL, int WR, int STAGES, bool F16, bool LT, bool RT>
+__device__ __forceinline__ void product_sums(const ProductArgs& a, const ProductPlace& at, f32x4 (&acc)[BL / WL / 16][BR / WR / 16]) {
     constexpr int T = 64 * WL * WR, NL = BL / WL / 16, NR = BR / WR / 16, STAGE = (BL + BR) * PK;
     extern __shared__ __align__(1024) uint16_t product_tiles[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wl = wave % WL, wr = wave / WL;
-    // Neighbouring tiles on one XCD: workgroups go to the XCDs in turn, so XCD x takes the x-th eighth of the tiles, in
-    // bands of 8 tiles of l, along r.
-    const int total = a.tiles_l * a.tiles_r * a.splits, per = (total + 7) >> 3;
-    const int id = (block & 7) * per + (block >> 3);
-    if ((block >> 3) >= per || id >= total) return;
-    const int per_split = a.tiles_l * a.tiles_r, split = id / per_split, in = id - split * per_split;
-    const int band = in / (8 * a.tiles_r), left = a.tiles_l - band * 8, height = left < 8 ? left : 8;
-    const int inb = in - band * 8 * a.tiles_r, tl = band * 8 + inb % height, tr = inb / height;
+    const int wl = wave % WL, wr = wave / WL, tl = at.tl, tr = at.tr, split = at.split;
 
-    f32x4 acc[NL][NR];
 #pragma unroll
     for (int i = 0; i < NL; ++i)
 #pragma unroll
@@ -268,22 +286,53 @@ __device__ __forceinline__ void product(const ProductArgs& a, const Epilogue& ep
         stage = after;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // nothing on its way to LDS, nobody reading
+}
+
+template <int BL, int BR, int WL, int WR, int STAGES, class Epilogue>
+__device__ __forceinline__ void product_finish(const ProductPlace& at, const Epilogue& epi, f32x4 (&acc)[BL / WL / 16][BR / WR / 16]) {
+    constexpr int NL = BL / WL / 16, NR = BR / WR / 16, STAGE = (BL + BR) * PK;
+    extern __shared__ __align__(1024) uint16_t product_tiles[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wl = wave % WL, wr = wave / WL;
     // (LDS in which an epilogue turns its values: a wavefront's own part)
     static_assert(!Epilogue::TURNS || NL * 16 * NR * 16 * WL * WR <= STAGES * STAGE, "the wavefronts' values fit");
     uint16_t* const own = product_tiles + wave * (NL * 16 * NR * 16);
-    epi.template finish<NL, NR>(acc, tl * BL + wl * (BL / WL), tr * BR + wr * (BR / WR), tr * WR + wr, split, lane, own);
+    epi.template finish<NL, NR>(acc, at.tl * BL + wl * (BL / WL), at.tr * BR + wr * (BR / WR), at.tr * WR + wr, at.split, lane, own);
 }
 
-template <int BL, int BR, int WL, int WR, int STAGES, bool F16, bool LT, bool RT, class Epilogue>
+template <int BL, int BR, int WL, int WR, int STAGES, bool LT, bool RT, class Epilogue>
+__device__ __forceinline__ void product(const ProductArgs& a, const Epilogue& epi, int block) {
+    ProductPlace at;
+    if (!product_place(a, block, at)) return;
+    f32x4 acc[BL / WL / 16][BR / WR / 16];
+    product_sums<BL, BR, WL, WR, STAGES, false, LT, RT>(a, at, acc);
+    product_finish<BL, BR, WL, WR, STAGES>(at, epi, acc);
+}
+
+template <int BL, int BR, int WL, int WR, int STAGES, bool LT, bool RT, class Epilogue>
 __global__ __launch_bounds__(64 * WL * WR) void product_kernel(ProductArgs a, Epilogue epi) {
-    product<BL, BR, WL, WR, STAGES, F16, LT, RT>(a, epi, blockIdx.x);
+    product<BL, BR, WL, WR, STAGES, LT, RT>(a, epi, blockIdx.x);
+}
+
+// Scores of fp32 rows, in the pieces that the rows ask for: of the same tiles, two fp16 ones (a16) or three bfloat16 ones (a3).
+template <int BL, int BR, int WL, int WR, int STAGES, class Epilogue>
+__global__ __launch_bounds__(64 * WL * WR) void score_kernel(ProductArgs a16, ProductArgs a3, const uint32_t* __restrict__ range, Epilogue epi) {
+    ProductPlace at;
+    if (!product_place(a16, blockIdx.x, at)) return;
+    f32x4 acc[BL / WL / 16][BR / WR / 16];
+    if (in_three_pieces(*range)) {
+        epi.back_l = epi.back_r = nullptr;
+        product_sums<BL, BR, WL, WR, STAGES, false, false, false>(a3, at, acc);
+    } else {
+        product_sums<BL, BR, WL, WR, STAGES, true, false, false>(a16, at, acc);
+    }
+    product_finish<BL, BR, WL, WR, STAGES>(at, epi, acc);
 }
 
 // Two products that do not depend on each other, in one launch: the first `blocks` workgroups (a multiple of 8) have one.
 template <int BL, int BR, int WL, int WR, int STAGES, bool LT1, bool RT1, bool LT2, bool RT2, class Epilogue>
 __global__ __launch_bounds__(64 * WL * WR) void product_pair_kernel(ProductArgs a1, Epilogue epi1, ProductArgs a2, Epilogue epi2, int blocks) {
-    if ((int)blockIdx.x < blocks) product<BL, BR, WL, WR, STAGES, false, LT1, RT1>(a1, epi1, blockIdx.x);
-    else product<BL, BR, WL, WR, STAGES, false, LT2, RT2>(a2, epi2, blockIdx.x - blocks);
+    if ((int)blockIdx.x < blocks) product<BL, BR, WL, WR, STAGES, LT1, RT1>(a1, epi1, blockIdx.x);
+    else product<BL, BR, WL, WR, STAGES, LT2, RT2>(a2, epi2, blockIdx.x - blocks);
 }
 
 }  // namespace qgbdt

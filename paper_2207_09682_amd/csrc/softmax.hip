@@ -68,8 +68,9 @@ __device__ __forceinline__ float common_weight(const LeftOut& src, int64_t rows)
 }
 
 // Up to WEIGHT_BLOCKS maxima of the rows' weights.  Bound by latency, with very many rows by memory (100,003 rows: 3 us).
-__global__ __launch_bounds__(256) void weight_kernel(LeftOut src, int64_t rows, uint32_t* __restrict__ tops) {
+__global__ __launch_bounds__(256) void weight_kernel(LeftOut src, int64_t rows, uint32_t* __restrict__ tops, uint32_t* __restrict__ range) {
     uint32_t top = 0;
+    if (range && blockIdx.x == 0 && threadIdx.x == 0) *range = 0;  // (for lay_out_fp32_kernel)
     const int64_t step = (int64_t)gridDim.x * 256;
 #pragma unroll 4
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows; i += step) { const uint32_t b = src.size_of_weight(i); top = b > top ? b : top; }
@@ -119,25 +120,46 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const typename E::T* __res
     }
 }
 
-// fp32 rows in two fp16 pieces for the scores, each row brought to 2^14 .. 2^15 by a power of two, which `back` undoes, and with `three` in
-// three bfloat16 pieces too, for the second products.  `lanes` threads have a row.  Bound by memory (100,003 x 64 with all pieces: 14 us, 6 TB/s).
-__global__ __launch_bounds__(256) void lay_out_fp32_kernel(const float* __restrict__ in, int64_t stride, int64_t rows, int dim, int dp, int lanes, uint16_t* __restrict__ halves,
-                                                           uint16_t* __restrict__ three, int64_t piece, float* __restrict__ back, LeftOut src) {
+constexpr int LAY_OUT_BLOCKS = 2048;  // workgroups per matrix: as many as the chip holds
+
+// A matrix of fp32 rows and where its pieces go.
+struct Fp32Rows {
+    const float* in;
+    int64_t stride, rows;
+    uint16_t* halves;  // two fp16 pieces, rows of dp values
+    uint16_t* three;   // three bfloat16 pieces, null in a loss
+    float* back;       // per row: takes scores of the fp16 pieces back
+};
+
+// fp32 rows in two fp16 pieces for the scores, each row brought to 2^14 .. 2^15 by a power of two, which `back` undoes, and with THREE in
+// three bfloat16 pieces too, for the second products.  `lanes` threads have a row.  The first w_blocks workgroups lay out the weights, the others x.  What
+// the rows say about their pieces (RANGE_...) goes to a byte per workgroup or into *range.  Bound by memory (100,003 x 64 with all pieces: 14 us, 6 TB/s).
+template <bool THREE>
+__global__ __launch_bounds__(256) void lay_out_fp32_kernel(Fp32Rows w, Fp32Rows x, int w_blocks, int dim, int dp, int lanes, LeftOut of_x, uint8_t* __restrict__ marks,
+                                                           uint32_t* __restrict__ range) {
+    __shared__ uint32_t found;
+    if (threadIdx.x == 0) found = 0;
+    const bool weights = (int)blockIdx.x < w_blocks;
+    const Fp32Rows m = weights ? w : x;
+    const LeftOut src = weights ? LeftOut{} : of_x;
+    const int block = (int)blockIdx.x - (weights ? 0 : w_blocks), blocks = weights ? w_blocks : (int)gridDim.x - w_blocks;
     const int sub = threadIdx.x & (lanes - 1), per = 256 / lanes;
-    const int64_t step = (int64_t)gridDim.x * per;
+    const int64_t step = (int64_t)blocks * per, rows = m.rows, piece = rows * dp;
     float unit = 1.0f;
-    if (src.terms || (src.common && blockIdx.x == 0)) {
+    if (src.terms || (src.common && block == 0)) {
         unit = common_weight(src, rows);
-        if (blockIdx.x == 0 && threadIdx.x == 0) *src.common = unit;
+        if (block == 0 && threadIdx.x == 0) *src.common = unit;
     }
+    __syncthreads();
+    uint32_t marked = 0;
     const int64_t filled = src.terms ? (rows + SWEEP_TILE - 1) / SWEEP_TILE * SWEEP_TILE : rows;
-    for (int64_t row = (int64_t)blockIdx.x * per + threadIdx.x / lanes; row < filled; row += step) {
+    for (int64_t row = (int64_t)block * per + threadIdx.x / lanes; row < filled; row += step) {
         if (row >= rows) {
             if (sub == 0) src.terms[row] = src.of(row, rows, unit, 1.0f);
             continue;
         }
         const bool live = src.live(row);
-        const float* const p = in + row * stride;
+        const float* const p = m.in + row * m.stride;
         uint32_t top = 0;  // bits of the largest magnitude: infinities and NaN are above all others
         for (int c = sub * 8; c < dim; c += lanes * 8) {
             const Eight<F32> v = load_eight<F32>(p, c, dim);
@@ -152,32 +174,90 @@ __global__ __launch_bounds__(256) void lay_out_fp32_kernel(const float* __restri
             top = b > top ? b : top;
         }
         const int e = (int)(top >> 23);
-        int shift = e == 255 || top == 0 || !live ? 0 : 14 + 127 - e;
+        const bool finite = e != 255 && top != 0 && live;  // (and not all zeros, which any pieces hold)
+        int shift = finite ? 14 + 127 - e : 0;
         if (shift > 120) shift = 120;
         const float by = __uint_as_float((uint32_t)(127 + shift) << 23), undo = __uint_as_float((uint32_t)(127 - shift) << 23);
         if (sub == 0) {
-            back[row] = undo;
+            m.back[row] = undo;
             if (src.terms) src.terms[row] = src.of(row, rows, unit, undo);
         }
+        const uint32_t large = top > (9u << 23) ? top - (9u << 23) : 0u, faint = top > (17u << 23) ? top - (17u << 23) : 0u;
+        int of_size = 0;
         for (int c = sub * 8; c < dp; c += lanes * 8) {
             const Eight<F32> v = load_eight<F32>(p, c, dim);
             union { uint16_t h[8]; uint4 q; } hi, lo, u[3];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const float value = live ? v.q[k / 4].v[k % 4] : 0.0f, x = value * by;
+                const uint32_t b = __float_as_uint(value) & 0x7fffffffu;
+                of_size += b >= large ? 1 : 0;
+                if (finite && b != 0 && b < faint) marked |= RANGE_FAINT;
                 hi.h[k] = to_f16(x);
                 const float r = x - from_f16(hi.h[k]);
                 lo.h[k] = fabsf(x) < __builtin_inff() ? to_f16(r) : 0;
-                uint16_t q[3];
-                three_pieces(value, q);
-                u[0].h[k] = q[0]; u[1].h[k] = q[1]; u[2].h[k] = q[2];
+                if constexpr (THREE) {
+                    uint16_t q[3];
+                    three_pieces(value, q);
+                    u[0].h[k] = q[0]; u[1].h[k] = q[1]; u[2].h[k] = q[2];
+                }
             }
-            *reinterpret_cast<uint4*>(halves + row * dp + c) = hi.q;
-            *reinterpret_cast<uint4*>(halves + piece + row * dp + c) = lo.q;
-            if (three)
+            *reinterpret_cast<uint4*>(m.halves + row * dp + c) = hi.q;
+            *reinterpret_cast<uint4*>(m.halves + piece + row * dp + c) = lo.q;
+            if constexpr (THREE)
 #pragma unroll
-                for (int s = 0; s < 3; ++s) *reinterpret_cast<uint4*>(three + s * piece + row * dp + c) = u[s].q;
+                for (int s = 0; s < 3; ++s) *reinterpret_cast<uint4*>(m.three + s * piece + row * dp + c) = u[s].q;
         }
+        for (int o = lanes >> 1; o > 0; o >>= 1) of_size += __shfl_xor(of_size, o);
+        if (finite && (dim - of_size) * 4 > dim) marked |= RANGE_LOOSE;
+        if (finite && (e < 127 - 50 || e > 127 + 50)) marked |= RANGE_WIDE;
+    }
+    if (marked) atomicOr(&found, marked);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        if (marks) marks[blockIdx.x] = (uint8_t)found;
+        else if (found) atomicOr(range, found);
+    }
+}
+
+// Between the layout and the scores of a loss: the range of all rows, and where it asks for them three bfloat16 pieces in place of the two of fp16.  before:
+// of the rows before these, whose pieces of the weights stay.
+__global__ __launch_bounds__(256) void settle_kernel(Fp32Rows w, Fp32Rows x, int dim, int dp, const uint8_t* __restrict__ marks, int n_marks, const uint32_t* __restrict__ before,
+                                                     uint32_t* __restrict__ range) {
+    __shared__ uint32_t found;
+    const uint32_t old = before ? *before : 0;
+    if (threadIdx.x == 0) found = old;
+    __syncthreads();
+    uint32_t marked = 0;
+    static_assert(2 * LAY_OUT_BLOCKS <= 16 * 256, "a thread has 16 bytes of the marks");
+    const int i0 = threadIdx.x * 16;
+    if (i0 < n_marks) {
+        union { uint4 q; uint8_t b[16]; } v;
+        v.q = *reinterpret_cast<const uint4*>(marks + i0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) marked |= i0 + i < n_marks ? v.b[i] : 0;
+    }
+    if (marked) atomicOr(&found, marked);
+    __syncthreads();
+    const uint32_t all = found;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *range = all;
+    if (!in_three_pieces(all)) return;
+    const int per_row = dp >> 3;
+    const int64_t of_w = in_three_pieces(old) ? 0 : w.rows * per_row, total = of_w + x.rows * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const Fp32Rows m = i < of_w ? w : x;
+        const int64_t j = i < of_w ? i : i - of_w, row = j / per_row;
+        const int c = (int)(j - row * per_row) * 8;
+        const Eight<F32> v = load_eight<F32>(m.in + row * m.stride, c, dim);
+        union { uint16_t h[8]; uint4 q; } u[3];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            uint16_t q[3];
+            three_pieces(v.q[k / 4].v[k % 4], q);
+            u[0].h[k] = q[0]; u[1].h[k] = q[1]; u[2].h[k] = q[2];
+        }
+#pragma unroll
+        for (int s = 0; s < 3; ++s) *reinterpret_cast<uint4*>(m.halves + s * m.rows * dp + row * dp + c) = u[s].q;
     }
 }
 
@@ -203,7 +283,7 @@ __device__ __forceinline__ void scale_back(f32x4 (&acc)[NL][NR], const float* ba
         }
 }
 
-// Maximum and sum of exponentials of a row's scores over a wavefront's strip of classes.  SCALED: of rows in fp16 pieces.
+// Maximum and sum of exponentials of a row's scores over a wavefront's strip of classes.  SCALED: of fp32 rows, in fp16 pieces where back_l is not null.
 template <bool SCALED>
 struct StatsEpilogue {
     float2* part;  // [rows][strips]
@@ -213,7 +293,7 @@ struct StatsEpilogue {
     static constexpr bool TURNS = false;
     template <int NL, int NR>
     __device__ __forceinline__ void finish(f32x4 (&acc)[NL][NR], int row0, int col0, int strip, int, int lane, uint16_t*) const {
-        if constexpr (SCALED) scale_back(acc, back_l, back_r, row0, col0, rows, cols, lane);
+        if (SCALED && back_l) scale_back(acc, back_l, back_r, row0, col0, rows, cols, lane);
         const int h4 = (lane >> 4) * 4;
         const bool whole = col0 + NR * 16 <= cols;
 #pragma unroll
@@ -543,18 +623,36 @@ static unsigned cut(ProductArgs& a, int tile, int64_t rows_l, int64_t rows_r) {
     return (unsigned)((a.tiles_l * a.tiles_r * a.splits + 7) / 8 * 8);
 }
 
-template <bool F16, bool LT, bool RT, class Epilogue>
+template <bool LT, bool RT, class Epilogue>
 static void launch_product(qgbdt_ctx* ctx, int tile, ProductArgs a, const Epilogue& e, int64_t rows_l, int64_t rows_r) {
     const dim3 grid(cut(a, tile, rows_l, rows_r));
     auto go = [&](auto kernel, int threads, int lds) {
         allow_lds(ctx, reinterpret_cast<const void*>(kernel), lds);
         hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, ctx->stream, a, e);
     };
-    if (tile == TILE_256) go(product_kernel<256, 256, 4, 2, 2, F16, LT, RT, Epilogue>, 512, product_lds(256, 256, 512, 2));
-    else if (tile == TILE_128) go(product_kernel<128, 128, 2, 2, 2, F16, LT, RT, Epilogue>, 256, product_lds(128, 128, 256, 2));
-    else if (tile == TILE_128x64) go(product_kernel<128, 64, 4, 1, 3, F16, LT, RT, Epilogue>, 256, product_lds(128, 64, 256, 3));
-    else if (tile == TILE_64) go(product_kernel<64, 64, 2, 2, 3, F16, LT, RT, Epilogue>, 256, product_lds(64, 64, 256, 3));
-    else if constexpr (!Epilogue::TURNS) go(product_kernel<32, 128, 1, 4, 6, F16, LT, RT, Epilogue>, 256, product_lds(32, 128, 256, 6));  // (D has 64 rows at least)
+    if (tile == TILE_256) go(product_kernel<256, 256, 4, 2, 2, LT, RT, Epilogue>, 512, product_lds(256, 256, 512, 2));
+    else if (tile == TILE_128) go(product_kernel<128, 128, 2, 2, 2, LT, RT, Epilogue>, 256, product_lds(128, 128, 256, 2));
+    else if (tile == TILE_128x64) go(product_kernel<128, 64, 4, 1, 3, LT, RT, Epilogue>, 256, product_lds(128, 64, 256, 3));
+    else if (tile == TILE_64) go(product_kernel<64, 64, 2, 2, 3, LT, RT, Epilogue>, 256, product_lds(64, 64, 256, 3));
+    else if constexpr (!Epilogue::TURNS) go(product_kernel<32, 128, 1, 4, 6, LT, RT, Epilogue>, 256, product_lds(32, 128, 256, 6));  // (D has 64 rows at least)
+}
+
+// Scores of fp32 rows; `three`: where their three bfloat16 pieces lie, of x and of the weights.
+template <class Epilogue>
+static void launch_scores(qgbdt_ctx* ctx, int tile, ProductArgs a, const uint16_t* three_l, const uint16_t* three_r, const uint32_t* range, const Epilogue& e, int64_t rows_l,
+                          int64_t rows_r) {
+    const dim3 grid(cut(a, tile, rows_l, rows_r));
+    ProductArgs b = a;
+    b.l.p = three_l; b.r.p = three_r; b.segs = 6; b.pieces_l = SIX_L; b.pieces_r = SIX_R;
+    auto go = [&](auto kernel, int threads, int lds) {
+        allow_lds(ctx, reinterpret_cast<const void*>(kernel), lds);
+        hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, ctx->stream, a, b, range, e);
+    };
+    if (tile == TILE_256) go(score_kernel<256, 256, 4, 2, 2, Epilogue>, 512, product_lds(256, 256, 512, 2));
+    else if (tile == TILE_128) go(score_kernel<128, 128, 2, 2, 2, Epilogue>, 256, product_lds(128, 128, 256, 2));
+    else if (tile == TILE_128x64) go(score_kernel<128, 64, 4, 1, 3, Epilogue>, 256, product_lds(128, 64, 256, 3));
+    else if (tile == TILE_64) go(score_kernel<64, 64, 2, 2, 3, Epilogue>, 256, product_lds(64, 64, 256, 3));
+    else if constexpr (!Epilogue::TURNS) go(score_kernel<32, 128, 1, 4, 6, Epilogue>, 256, product_lds(32, 128, 256, 6));
 }
 
 // Whether the products read fp32 weights where they lie (middle_device.h).  Scores of pieces that are made once take half the products: the loss of
@@ -673,7 +771,7 @@ struct SoftmaxPlan {
     bool x_slabs, w_slabs;
     int64_t ld_d, slab_ld;
     // offsets in the scratch block
-    size_t common, tops, terms, x16, w16, x_back, w_back, x, w, part, d, xs, ws, bytes;
+    size_t common, tops, range, marks, terms, x16, w16, x_back, w_back, x, w, part, d, xs, ws, bytes;
 };
 
 static SoftmaxPlan make_softmax_plan(int64_t n, int dim, int64_t n_classes, int dtype, int64_t x_stride, int64_t w_stride, bool gradients) {
@@ -691,8 +789,12 @@ static SoftmaxPlan make_softmax_plan(int64_t n, int dim, int64_t n_classes, int 
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
     const bool halves = p.pieces > 1 && !p.few && !p.middle;  // scores of rows in fp16 pieces
+    // (the loss has room for the three bfloat16 pieces in the place of the fp16 ones)
+    const size_t half_bytes = gradients ? 4 : 6;
     if (halves) {
-        p.w16 = take((size_t)n_classes * p.dp * 4);
+        p.range = take(8);
+        p.marks = take(2 * LAY_OUT_BLOCKS);
+        p.w16 = take((size_t)n_classes * p.dp * half_bytes);
         p.w_back = take((size_t)((n_classes + SWEEP_TILE - 1) / SWEEP_TILE * SWEEP_TILE) * 4);
     }
     // (the loss reads no other pieces than those)
@@ -701,7 +803,7 @@ static SoftmaxPlan make_softmax_plan(int64_t n, int dim, int64_t n_classes, int 
     p.row_blocks = n > 0 ? (n + p.row_block - 1) / p.row_block : 0;
     if (!gradients) {
         if (halves) {
-            p.x16 = take((size_t)p.row_block * p.dp * 4);
+            p.x16 = take((size_t)p.row_block * p.dp * half_bytes);
             p.x_back = take((size_t)p.row_block * 4);
         }
         p.x = p.copy_x && !halves ? take((size_t)p.row_block * p.dp * 2 * p.pieces) : 0;
@@ -797,12 +899,21 @@ static void lay_out(qgbdt_ctx* ctx, const SoftmaxPlan& p, const void* in, int64_
                            src);
 }
 
-static void lay_out_fp32(qgbdt_ctx* ctx, const SoftmaxPlan& p, const void* in, int64_t stride, int64_t rows, int dim, void* halves, void* three, void* back, const LeftOut& src = {}) {
-    int lanes = 1;
-    while (lanes < 64 && lanes * 8 < p.dp) lanes <<= 1;
-    const int64_t blocks = (rows + 256 / lanes - 1) / (256 / lanes);
-    hipLaunchKernelGGL(lay_out_fp32_kernel, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, ctx->stream, static_cast<const float*>(in), stride, rows, dim, p.dp, lanes,
-                       static_cast<uint16_t*>(halves), static_cast<uint16_t*>(three), rows * p.dp, static_cast<float*>(back), src);
+// Workgroups that lay out `rows` rows.
+static int lay_out_blocks(int dp, int64_t rows, int* lanes) {
+    *lanes = 1;
+    while (*lanes < 64 && *lanes * 8 < dp) *lanes <<= 1;
+    const int64_t blocks = (rows + 256 / *lanes - 1) / (256 / *lanes);
+    return (int)(blocks < LAY_OUT_BLOCKS ? blocks : LAY_OUT_BLOCKS);
+}
+
+// w.rows = 0: x alone
+static void lay_out_fp32(qgbdt_ctx* ctx, const SoftmaxPlan& p, const Fp32Rows& w, const Fp32Rows& x, int dim, const LeftOut& of_x, uint8_t* marks, uint32_t* range) {
+    int lanes;
+    const int w_blocks = lay_out_blocks(p.dp, w.rows, &lanes), x_blocks = lay_out_blocks(p.dp, x.rows, &lanes);
+    const dim3 grid((unsigned)(w_blocks + x_blocks));
+    if (x.three) hipLaunchKernelGGL(lay_out_fp32_kernel<true>, grid, dim3(256), 0, ctx->stream, w, x, w_blocks, dim, p.dp, lanes, of_x, marks, range);
+    else hipLaunchKernelGGL(lay_out_fp32_kernel<false>, grid, dim3(256), 0, ctx->stream, w, x, w_blocks, dim, p.dp, lanes, of_x, marks, range);
 }
 
 template <class E, int PIECES, int MODE>
@@ -827,8 +938,9 @@ int run_softmax_loss(qgbdt_ctx* ctx, const void* x, const void* w, int dtype, in
     const bool halves = p.pieces > 1 && !p.few && !p.middle;
     ProductArgs a = {};
     a.r = {static_cast<const uint16_t*>(w), w_stride, 0, (int)n_classes, p.dp};
+    const Fp32Rows of_w = {static_cast<const float*>(w), w_stride, n_classes, reinterpret_cast<uint16_t*>(s + p.w16), nullptr, reinterpret_cast<float*>(s + p.w_back)};
+    uint32_t* range = reinterpret_cast<uint32_t*>(s + p.range);
     if (halves) {
-        lay_out_fp32(ctx, p, w, w_stride, n_classes, dim, s + p.w16, nullptr, s + p.w_back);
         a.r = {reinterpret_cast<const uint16_t*>(s + p.w16), p.dp, n_classes * p.dp, (int)n_classes, p.dp};
     } else if (p.copy_w) {
         lay_out(ctx, p, w, w_stride, n_classes, dim, s + p.w);
@@ -844,7 +956,19 @@ int run_softmax_loss(qgbdt_ctx* ctx, const void* x, const void* w, int dtype, in
         const char* const tg = static_cast<const char*>(target) + r0 * target_bytes;
         a.l = {reinterpret_cast<const uint16_t*>(xb), x_stride, 0, (int)rows, p.dp};
         if (halves) {
-            lay_out_fp32(ctx, p, xb, x_stride, rows, dim, s + p.x16, nullptr, s + p.x_back);
+            const Fp32Rows of_x = {reinterpret_cast<const float*>(xb), x_stride, rows, reinterpret_cast<uint16_t*>(s + p.x16), nullptr, reinterpret_cast<float*>(s + p.x_back)};
+            int lanes;
+            uint8_t* const marks = s + p.marks;
+            const int w_blocks = lay_out_blocks(p.dp, n_classes, &lanes), x_blocks = lay_out_blocks(p.dp, rows, &lanes);
+            Fp32Rows w_now = of_w;
+            if (r0 > 0) w_now.rows = 0;  // (laid out already)
+            lay_out_fp32(ctx, p, w_now, of_x, dim, LeftOut{}, marks + (r0 > 0 ? w_blocks : 0), nullptr);
+            // (the range in two words by turns: that of the rows before these is read)
+            const uint32_t* const before = r0 > 0 ? range : nullptr;
+            range = reinterpret_cast<uint32_t*>(s + p.range) + (r0 / p.row_block & 1);
+            const int blocks = stream_blocks((n_classes + rows) * (p.dp / 8));
+            hipLaunchKernelGGL(settle_kernel, dim3(blocks < 1024 ? blocks : 1024), dim3(256), 0, ctx->stream, of_w, of_x, dim, p.dp, marks, w_blocks + x_blocks,
+                               before, range);
             a.l = {reinterpret_cast<const uint16_t*>(s + p.x16), p.dp, rows * p.dp, (int)rows, p.dp};
         } else if (p.copy_x) {
             lay_out(ctx, p, xb, x_stride, rows, dim, s + p.x);
@@ -864,13 +988,13 @@ int run_softmax_loss(qgbdt_ctx* ctx, const void* x, const void* w, int dtype, in
             SweepArgs v = {};
             v.kept = a.l.p; v.kept_ld = a.l.ld; v.kept_piece = a.l.piece; v.n_kept = (int)rows;
             v.swept = a.r.p; v.swept_ld = a.r.ld; v.swept_piece = a.r.piece; v.n_swept = (int)n_classes;
-            v.dp = p.dp; v.splits = (int)p.strips; v.part = part; v.kept_back = x_back; v.swept_back = w_back;
+            v.dp = p.dp; v.splits = (int)p.strips; v.part = part; v.kept_back = x_back; v.swept_back = w_back; v.range = range;
             if (halves) launch_sweep<F32, 3, SWEEP_STATS>(ctx, p.sweep, v);
             else launch_sweep<BF16, 1, SWEEP_STATS>(ctx, p.sweep, v);
         } else if (halves) {
-            launch_product<true, false, false>(ctx, p.tile, a, StatsEpilogue<true>{part, (int)p.strips, (int)rows, (int)n_classes, x_back, w_back}, rows, n_classes);
+            launch_scores(ctx, p.tile, a, a.l.p, a.r.p, range, StatsEpilogue<true>{part, (int)p.strips, (int)rows, (int)n_classes, x_back, w_back}, rows, n_classes);
         } else {
-            launch_product<false, false, false>(ctx, p.tile, a, StatsEpilogue<false>{part, (int)p.strips, (int)rows, (int)n_classes, nullptr, nullptr}, rows, n_classes);
+            launch_product<false, false>(ctx, p.tile, a, StatsEpilogue<false>{part, (int)p.strips, (int)rows, (int)n_classes, nullptr, nullptr}, rows, n_classes);
         }
         const dim3 grid((unsigned)((rows + 3) / 4));
         if (dtype == QGBDT_F32)
@@ -903,20 +1027,29 @@ static void gradients(qgbdt_ctx* ctx, const SoftmaxPlan& p, const typename E::T*
     int64_t w_ld = w_stride, w_piece = 0;
     const bool halves = PIECES > 1 && !p.few && !p.middle;
     if (p.copy_w) {
-        if (halves) lay_out_fp32(ctx, p, w, w_stride, n_classes, dim, s + p.w16, s + p.w, s + p.w_back);
-        else lay_out(ctx, p, w, w_stride, n_classes, dim, s + p.w);
+        if (!halves) lay_out(ctx, p, w, w_stride, n_classes, dim, s + p.w);
         wp = reinterpret_cast<const uint16_t*>(s + p.w); w_ld = p.dp; w_piece = n_classes * p.dp;
     }
     const uint16_t* const xp = reinterpret_cast<const uint16_t*>(s + p.x);
     const uint16_t *const x16 = reinterpret_cast<const uint16_t*>(s + p.x16), *const w16 = reinterpret_cast<const uint16_t*>(s + p.w16);
     const float *const x_back = reinterpret_cast<const float*>(s + p.x_back), *const w_back = reinterpret_cast<const float*>(s + p.w_back);
-    uint32_t* const tops = n > WEIGHTS_AT_ONCE ? reinterpret_cast<uint32_t*>(s + p.tops) : nullptr;
+    uint32_t* const tops = n > WEIGHTS_AT_ONCE || halves ? reinterpret_cast<uint32_t*>(s + p.tops) : nullptr;
     const int n_tops = (int)(n < WEIGHT_BLOCKS * 1024 ? (n + 1023) / 1024 : WEIGHT_BLOCKS);
-    if (tops) hipLaunchKernelGGL(weight_kernel, dim3(n_tops), dim3(256), 0, ctx->stream, LeftOut{target, target_bytes, n_classes, weight, lse, nullptr, 0, nullptr, nullptr}, n, tops);
+    uint32_t* const range = halves ? reinterpret_cast<uint32_t*>(s + p.range) : nullptr;
+    if (tops)
+        hipLaunchKernelGGL(weight_kernel, dim3(n_tops), dim3(256), 0, ctx->stream, LeftOut{target, target_bytes, n_classes, weight, lse, nullptr, 0, nullptr, nullptr}, n,
+                           tops, range);
     auto lay_out_x = [&](int64_t r0, int64_t rows, float* common, RowTerms* terms) {
         const LeftOut src = {static_cast<const char*>(target) + r0 * target_bytes, target_bytes, n_classes, weight + r0, lse + r0, tops, n_tops, common, terms};
-        if (halves) lay_out_fp32(ctx, p, x + r0 * x_stride, x_stride, rows, dim, s + p.x16, s + p.x, s + p.x_back, src);
-        else lay_out(ctx, p, x + r0 * x_stride, x_stride, rows, dim, s + p.x, src);
+        if constexpr (PIECES > 1) {
+            if (halves) {  // (with the first rows the weights)
+                const Fp32Rows of_w = {w, w_stride, r0 ? 0 : n_classes, reinterpret_cast<uint16_t*>(s + p.w16), reinterpret_cast<uint16_t*>(s + p.w), reinterpret_cast<float*>(s + p.w_back)};
+                const Fp32Rows of_x = {x + r0 * x_stride, x_stride, rows, reinterpret_cast<uint16_t*>(s + p.x16), reinterpret_cast<uint16_t*>(s + p.x), reinterpret_cast<float*>(s + p.x_back)};
+                lay_out_fp32(ctx, p, of_w, of_x, dim, src, nullptr, range);
+                return;
+            }
+        }
+        lay_out(ctx, p, x + r0 * x_stride, x_stride, rows, dim, s + p.x, src);
     };
     if (p.few) {
         float* const common = reinterpret_cast<float*>(s + p.common);
@@ -942,16 +1075,16 @@ static void gradients(qgbdt_ctx* ctx, const SoftmaxPlan& p, const typename E::T*
         RowTerms* const terms = reinterpret_cast<RowTerms*>(s + p.terms);
         lay_out_x(0, n, common, terms);
         SweepArgs v = {};
-        v.dp = p.dp; v.dim = dim; v.terms = terms; v.unit = common; v.slab_ld = p.slab_ld;
+        v.dp = p.dp; v.dim = dim; v.terms = terms; v.unit = common; v.slab_ld = p.slab_ld; v.range = range;
         if (grad_x) {
-            v.kept = PIECES > 1 ? x16 : xp; v.kept_ld = p.dp; v.kept_piece = n * p.dp; v.n_kept = (int)n; v.swept16 = w16; v.kept_back = x_back; v.swept_back = w_back;
+            v.kept = xp; v.kept16 = x16; v.kept_ld = p.dp; v.kept_piece = n * p.dp; v.n_kept = (int)n; v.swept16 = w16; v.kept_back = x_back; v.swept_back = w_back;
             v.swept = wp; v.swept_ld = w_ld; v.swept_piece = w_piece; v.n_swept = (int)n_classes;
             v.splits = p.x_splits; v.out = grad_x; v.slab = p.x_slabs ? reinterpret_cast<float*>(s + p.xs) : nullptr; v.slab_size = n * p.slab_ld;
             launch_sweep<E, PIECES, SWEEP_ROWS>(ctx, p.sweep, v);
             if (v.slab) join_slabs<E>(ctx, v.slab, v.slab_size, p.slab_ld, p.x_splits, n, dim, grad_x, common);
         }
         if (grad_w) {
-            v.kept = PIECES > 1 ? w16 : wp; v.kept_ld = PIECES > 1 ? p.dp : w_ld; v.kept_piece = n_classes * p.dp; v.n_kept = (int)n_classes; v.swept16 = x16; v.kept_back = w_back;
+            v.kept = wp; v.kept16 = w16; v.kept_ld = w_ld; v.kept_piece = n_classes * p.dp; v.n_kept = (int)n_classes; v.swept16 = x16; v.kept_back = w_back;
             v.swept = xp; v.swept_ld = p.dp; v.swept_piece = n * p.dp; v.n_swept = (int)n;
             v.splits = p.w_splits; v.out = grad_w; v.slab = p.w_slabs ? reinterpret_cast<float*>(s + p.ws) : nullptr; v.slab_size = n_classes * p.slab_ld;
             launch_sweep<E, PIECES, SWEEP_CLASSES>(ctx, p.sweep, v);
@@ -988,7 +1121,9 @@ static void gradients(qgbdt_ctx* ctx, const SoftmaxPlan& p, const typename E::T*
             g.rows = (int)rows; g.rows_out = (int)rows_out; g.cols = (int)cols; g.cols_out = (int)cols_out; g.first = c0; g.n_classes = n_classes;
             if (!p.middle) {
                 g.back_l = x_back; g.back_r = w_back + c0;
-                launch_product<(PIECES > 1), false, false>(ctx, pick_tile(rows_out, cols_out, a.steps * a.segs), a, g, rows_out, cols_out);
+                const int tile = pick_tile(rows_out, cols_out, a.steps * a.segs);
+                if constexpr (PIECES > 1) launch_scores(ctx, tile, a, xp, wp + c0 * w_ld, range, g, rows_out, cols_out);
+                else launch_product<false, false>(ctx, tile, a, g, rows_out, cols_out);
             }
             // dX += D W, dW of the strip (+)= D^T X
             ProductArgs ax = base, aw = base;
@@ -1017,13 +1152,13 @@ static void gradients(qgbdt_ctx* ctx, const SoftmaxPlan& p, const typename E::T*
                 }
             }
             if (p.middle) {
-                if (grad_w) launch_product<false, true, true>(ctx, tw, aw, ew, cols, dim);
+                if (grad_w) launch_product<true, true>(ctx, tw, aw, ew, cols, dim);
             } else if (grad_x && grad_w && bx + bw <= 1024 && (int64_t)ax.steps * ax.segs <= 16 * ax.splits && (int64_t)aw.steps * aw.segs <= 16 * aw.splits) {
                 hipLaunchKernelGGL((product_pair_kernel<64, 64, 2, 2, 3, false, true, true, true, StoreEpilogue<E>>), dim3(bx + bw), dim3(256), product_lds(64, 64, 256, 3),
                                    ctx->stream, sx, ex, sw, ew, (int)bx);
             } else {
-                if (grad_x) launch_product<false, false, true>(ctx, tx, ax, ex, rows, dim);
-                if (grad_w) launch_product<false, true, true>(ctx, tw, aw, ew, cols, dim);
+                if (grad_x) launch_product<false, true>(ctx, tx, ax, ex, rows, dim);
+                if (grad_w) launch_product<true, true>(ctx, tw, aw, ew, cols, dim);
             }
             if (grad_w && slab && b == p.row_blocks - 1) join_slabs<E>(ctx, slab, ws_rows * p.slab_ld, p.slab_ld, p.w_splits, cols, dim, grad_w + c0 * dim, common);
         }

@@ -27,9 +27,10 @@ struct RowTerms {
 struct SweepArgs {
     const uint16_t *kept, *swept;  // rows of 8-element pieces
     int64_t kept_ld, swept_ld, kept_piece, swept_piece;
-    // fp32 rows: the scores are those of two fp16 pieces, which `kept` is in, and `swept` for STATS; else `swept` is in three bfloat16 pieces for
-    // the second product, and swept16 (rows of dp values, pieces n_swept rows apart) for the scores
-    const uint16_t* swept16;
+    // fp32 rows: `kept`, and `swept` for STATS, are in the pieces that the scores are made of, which `range` says; else `swept` is in three bfloat16
+    // pieces for the second product, swept16 and kept16 are in two fp16 ones for the scores (rows of dp values, pieces a matrix apart)
+    const uint16_t *swept16, *kept16;
+    const uint32_t* range;
     const float *kept_back, *swept_back;  // (CLASSES: the swept rows' are in their terms)
     int n_kept, n_swept, dp;       // dp: values of a row that exist, a multiple of 8
     int tiles, splits;             // workgroups along the kept rows; parts of the swept ones
@@ -50,28 +51,29 @@ __device__ __forceinline__ int swept_turn(int row) {
     return CB == 8 ? ((row >> 1) & 3) << 1 : (row & 7) << 1;
 }
 
-// Pieces of a swept row in LDS: for the scores, and behind them for the second product where those are others.
-template <int PIECES, int MODE>
+// Pieces of a swept row in LDS: for the scores, and behind them for the second product where those are others.  HALVES: fp32 rows whose scores are of
+// two fp16 pieces.
+template <int PIECES, int MODE, bool HALVES>
 struct SweepPieces {
-    static constexpr bool F16 = PIECES == 3;
-    static constexpr int SCORE = F16 ? 2 : 1, SECOND = MODE == SWEEP_STATS ? 0 : PIECES, ALL = F16 ? SCORE + SECOND : 1;
+    static constexpr bool F16 = HALVES;
+    static constexpr int SCORE = F16 ? 2 : PIECES, SECOND = MODE == SWEEP_STATS ? 0 : PIECES, ALL = F16 ? SCORE + SECOND : PIECES;
     static constexpr int SECOND_AT = F16 ? SCORE : 0;
     static constexpr bool TERMS = MODE == SWEEP_CLASSES, BACK = F16 && MODE != SWEEP_CLASSES;
 };
 // Swept rows per step (32 where the tile of 64 would leave LDS for two stages only), stages, bytes of LDS (1 KB of each for the rows' terms).
-template <int DP, int PIECES, int MODE>
+template <int DP, int PIECES, int MODE, bool HALVES>
 struct SweepShape {
-    typedef SweepPieces<PIECES, MODE> P;
+    typedef SweepPieces<PIECES, MODE, HALVES> P;
     static constexpr int TILE = P::ALL * 64 * DP * 2 * 3 > 150 * 1024 ? 32 : 64;
     static constexpr int STAGES = 3;
     static constexpr int TERMS = P::ALL * TILE * DP, STAGE = TERMS + (P::TERMS || P::BACK ? 512 : 0);  // elements
     static constexpr int LDS = STAGES * STAGE * 2;
 };
 
-template <class E, int DP, int PIECES, int MODE>
-__global__ __launch_bounds__(512) void sweep_kernel(SweepArgs a) {
-    typedef SweepPieces<PIECES, MODE> SP;
-    typedef SweepShape<DP, PIECES, MODE> SH;
+template <class E, int DP, int PIECES, int MODE, bool HALVES>
+__device__ __forceinline__ void sweep(const SweepArgs& a) {
+    typedef SweepPieces<PIECES, MODE, HALVES> SP;
+    typedef SweepShape<DP, PIECES, MODE, HALVES> SH;
     constexpr int CB = DP / 8, NK = DP / 32, NM = DP / 16, TILE = SH::TILE, STAGES = SH::STAGES, STAGE = SH::STAGE, TERMS = SH::TERMS;
     constexpr int ROUNDS = SP::ALL * TILE * CB / 512, LOADS = ROUNDS + (SP::TERMS || SP::BACK ? 1 : 0);
     static_assert(TILE * CB % 512 == 0, "a round's loads are of one piece");
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(512) void sweep_kernel(SweepArgs a) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int row = kept0 + i * 16 + s;
-        const uint16_t* const p = a.kept + (int64_t)(row < a.n_kept ? row : a.n_kept - 1) * a.kept_ld + g * 8;
+        const uint16_t* const p = (SP::F16 && MODE != SWEEP_STATS ? a.kept16 : a.kept) + (int64_t)(row < a.n_kept ? row : a.n_kept - 1) * a.kept_ld + g * 8;
 #pragma unroll
         for (int k = 0; k < NK; ++k)
 #pragma unroll
@@ -192,12 +194,14 @@ __global__ __launch_bounds__(512) void sweep_kernel(SweepArgs a) {
 #pragma unroll
                 for (int q = 0; q < SP::SCORE; ++q)
                     y[j][q] = *reinterpret_cast<const bf16x8*>(tile + (q * TILE + (h * 2 + j) * 16 + s) * DP + (((k * 4 + g) ^ swept_turn<CB>(s)) << 3));
+            constexpr int PRODUCTS = SP::SCORE == 3 ? 6 : SP::SCORE == 2 ? 3 : 1;  // (of pieces, smallest first)
+            constexpr uint32_t OF_L = SP::SCORE == 3 ? SIX_L : SP::SCORE == 2 ? THREE_R : 0, OF_R = SP::SCORE == 3 ? SIX_R : SP::SCORE == 2 ? THREE_L : 0;
 #pragma unroll
-            for (int p = SP::F16 ? 0 : 2; p < 3; ++p)  // (lo hi, hi lo, hi hi)
+            for (int p = 0; p < PRODUCTS; ++p)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) acc[i][j] = matrix_product<SP::F16>(y[j][p == 0 ? SP::SCORE - 1 : 0], x[i][k][p == 1 ? SP::SCORE - 1 : 0], acc[i][j]);
+                    for (int i = 0; i < 2; ++i) acc[i][j] = matrix_product<SP::F16>(y[j][(OF_R >> (4 * p)) & 0xf], x[i][k][(OF_L >> (4 * p)) & 0xf], acc[i][j]);
         }
     };
     // what becomes of them: the running maximum and sum, or D as an operand
@@ -389,7 +393,20 @@ __global__ __launch_bounds__(512) void sweep_kernel(SweepArgs a) {
     }
 }
 
+template <class E, int DP, int PIECES, int MODE>
+__global__ __launch_bounds__(512) void sweep_kernel(SweepArgs a) {
+    if constexpr (PIECES == 3) {
+        if (in_three_pieces(*a.range)) sweep<E, DP, PIECES, MODE, false>(a);
+        else sweep<E, DP, PIECES, MODE, true>(a);
+    } else {
+        sweep<E, DP, PIECES, MODE, false>(a);
+    }
+}
+
 template <int DP, int PIECES, int MODE>
-constexpr int sweep_lds() { return SweepShape<DP, PIECES, MODE>::LDS; }
+constexpr int sweep_lds() {
+    constexpr int halves = PIECES == 3 ? SweepShape<DP, PIECES, MODE, PIECES == 3>::LDS : 0, all = SweepShape<DP, PIECES, MODE, false>::LDS;
+    return halves > all ? halves : all;
+}
 
 }  // namespace qgbdt

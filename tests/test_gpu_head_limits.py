@@ -15,11 +15,12 @@ BF16_SHAPES = [(3, 40, 500), (9, 264, 3000), (16, 512, 130), (60, 64, 500), (200
 
 
 def _gradients_fit(x, w, u, got, gx, gw, smag, pu, d, lse):
-    """The bound of test_softmax_loss_and_gradients on both gradients (None: not looked at)."""
+    """The bound of test_softmax_loss_and_gradients on both gradients (None: not looked at), and for what fp32 cannot hold of D in units of the largest weight: below 2^-126
+    it may hold nothing."""
     dtype = x.dtype
     serr = 32 * U * smag.amax(1)
     perr = (2 * serr + 64 * U * (2 + smag.amax(1) + lse.abs())).unsqueeze(1) * pu
-    e = perr + ((2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -23) + 32 * U) * d.abs()
+    e = perr + ((2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -23) + 32 * U) * d.abs() + 2.0 ** -126 * float(u.abs().max())
     r = ROUND[dtype]
     if got[0] is not None:
         assert bool(((got[0].cpu().double() - gx).abs() <= r * gx.abs() + e @ w.double().abs() + 1e-30).all())
@@ -86,3 +87,94 @@ def test_the_rows_that_count_come_last(ctx, dtype, dim):  # noqa: F811
     _, want_lse, gx, gw, smag, pu, d, ok = _definition(x, w, t, u)
     assert bool((got[0][:n - live] == 0).all())
     _gradients_fit(x, w, u, (got[0][n - live:], got[1]), gx, gw, smag, pu, d, want_lse)
+
+
+# ---- fp32 scores of rows whose values differ much in size ------------------------------------------------
+
+
+def _uneven(n, dim, vocab, kind):
+    """fp32 rows whose scores are sums of terms of one size, or of few terms, while the rows themselves range over many orders of magnitude."""
+    x, w, t, u = _problem(n, dim, vocab, torch.float32)
+    g = _gen(n + dim)
+    if kind == "one column":  # 1e8 times larger in x and as much smaller in the weights
+        x[:, 3] *= 1e8
+        w[:, 3] *= 1e-8
+    elif kind == "columns":  # powers of ten from -15 to 15
+        f = 10.0 ** (30.0 * torch.rand(dim, generator=g, dtype=torch.float64) - 15.0)
+        x, w = (x.double() * f).float(), (w.double() / f).float()
+    elif kind == "rows of their own":  # each row has its large value where the weights are small
+        at = torch.randint(0, dim // 4, (n,), generator=g)
+        x[torch.arange(n), at] *= 1e9
+        w[:, :dim // 4] *= 1e-9
+    elif kind == "one value":  # of each row of x, which meets a small value of every class
+        at = torch.randint(0, dim - 1, (n,), generator=g)
+        x = torch.zeros_like(x)
+        x[torch.arange(n), at] = 1e10 * torch.rand(n, generator=g)
+        w[:, dim - 1] *= 1e10
+        w *= 1e-10
+    elif kind == "wide":  # scores of 1e4, which scaled back by one of the rows' powers of two alone are beyond fp32
+        x, w = x * 1e37, w * 1e-33
+    return x, w, t, u
+
+
+UNEVEN = ["one column", "columns", "rows of their own", "one value", "wide"]
+UNEVEN_SHAPES = [(16, 72, 300), (40, 512, 130), (60, 64, 500), (200, 100, 700), (3000, 128, 300), (100, 192, 3000), (300, 520, 1000), (600, 136, 8300), (2100, 264, 2300), (1300, 1032, 3000)]
+
+
+@pytest.mark.parametrize("kind", UNEVEN)
+@pytest.mark.parametrize("n,dim,vocab", UNEVEN_SHAPES)
+def test_fp32_scores_of_uneven_rows(ctx, n, dim, vocab, kind):  # noqa: F811
+    """The bounds of test_softmax_loss_and_gradients, which go by the sum of a score's magnitudes, whatever the rows' own range is."""
+    x, w, t, u = _uneven(n, dim, vocab, kind)
+    loss, lse, gx, gw, smag, pu, d, ok = _definition(x, w, t, u)
+    got_loss, got_lse = ctx.softmax_loss(x.cuda(), w.cuda(), t.cuda())
+    serr = 32 * U * smag.amax(1)
+    assert bool(((got_lse.cpu().double() - lse).abs() <= serr + 32 * U * (1 + lse.abs())).all())
+    assert bool(((got_loss.cpu().double() - loss).abs() <= 2 * serr + 32 * U * (1 + lse.abs() + smag.amax(1))).all())
+    _gradients_fit(x, w, u, ctx.softmax_gradients(x.cuda(), w.cuda(), t.cuda(), got_lse, u.cuda()), gx, gw, smag, pu, d, lse)
+
+
+@pytest.mark.parametrize("n,dim,vocab,at", [(131_200, 132, 20, 131_150), (131_200, 132, 20, 7), (300_000, 40, 24, 290_000)])
+def test_one_uneven_row_among_blocks_of_rows(ctx, n, dim, vocab, at):  # noqa: F811
+    """Of rows that are taken in blocks, one in the last block, or in the first, asks for other pieces than the rest."""
+    x, w, t, u = _problem(n, dim, vocab, torch.float32)
+    w[:, 2] *= 1e-9
+    x[at] *= 0.25
+    x[at, 2] = 3e8
+    got_loss, got_lse = (a.cpu().double() for a in ctx.softmax_loss(x.cuda(), w.cuda(), t.cuda()))
+    some = torch.cat([torch.arange(100), torch.arange(at - 7, at + 50), torch.arange(n - 50, n)])
+    loss, lse, gx, gw, smag, pu, d, ok = _definition(x[some], w, t[some], u[some])
+    serr = 32 * U * smag.amax(1)
+    assert bool(((got_lse[some] - lse).abs() <= serr + 32 * U * (1 + lse.abs())).all())
+    assert bool(((got_loss[some] - loss).abs() <= 2 * serr + 32 * U * (1 + lse.abs() + smag.amax(1))).all())
+    g = ctx.softmax_gradients(x.cuda(), w.cuda(), t.cuda(), got_lse.float().cuda(), u.cuda())
+    _gradients_fit(x[some], w, u[some], (g[0].cpu()[some], None), gx, gw, smag, pu, d, lse)
+
+
+@pytest.mark.parametrize("kind", ["even", "one column"])
+@pytest.mark.parametrize("n,dim,vocab", [(16, 72, 2), (60, 64, 2), (200, 128, 2), (100, 192, 2), (2500, 264, 520), (70_000, 136, 24)])
+def test_no_piece_of_fp32_values_is_lost(ctx, n, dim, vocab, kind):  # noqa: F811
+    """Positive values whose second and third pieces all have one sign, so that a product of pieces that is left out or taken twice adds up: 2^-9 of a score or
+    2^-17 of it.  Two classes have weights and the rest a tenth of them, so the log of the normaliser shows the scores, and the gradients' sums have few large terms.
+    Bounds: 6 u of the sum of magnitudes for a score (roundings of dim / 32 partial sums and of the pieces, at random), 16 u where pieces are of fp16,
+    twice that for a gradient that has the score's error and its own."""
+    g = _gen(dim)
+    tail = 1.0 + 0.2 * 2.0 ** -8 + 0.2 * 2.0 ** -16  # (to the nearest 8 bits: 1, rest 0.2 * 2^-8 and so on)
+    grid = lambda *s: 0.25 * (1.0 + torch.randint(0, 128, s, generator=g) / 128.0) * (1.0 + 0.0 * torch.rand(s, generator=g))  # noqa: E731
+    x, w = (grid(n, dim).double() * tail).float(), (grid(vocab, dim).double() * tail).float()
+    w[2:] = -w[2:]
+    if kind == "one column":
+        x[:, 5] *= 2.0 ** 26
+        w[:, 5] *= 2.0 ** -26
+        x[:, 6] *= 2.0 ** -26
+        w[:, 6] *= 2.0 ** 26
+    t, u = torch.arange(n) % 2, torch.ones(n)
+    loss, lse, gx, gw, smag, pu, d, ok = _definition(x, w, t, u)
+    got_loss, got_lse = ctx.softmax_loss(x.cuda(), w.cuda(), t.cuda())
+    top = smag[:, :2].amax(1)
+    assert bool(((got_lse.cpu().double() - lse).abs() <= 16 * U * (top + 1)).all())
+    got = ctx.softmax_gradients(x.cuda(), w.cuda(), t.cuda(), got_lse, u.cuda())
+    # p (1 - p) at most 1/4 times the error of s - lse, both classes
+    perr = 32 * U * (top + 1)[:, None] * (pu * (1 - pu) + 1e-12) + 8 * U * d.abs()
+    assert bool(((got[0].cpu().double() - gx).abs() <= perr @ w.double().abs() + 8 * U * (d.abs() @ w.double().abs()) + 1e-30).all())
+    assert bool(((got[1].cpu().double() - gw).abs() <= perr.t() @ x.double().abs() + 8 * U * (d.abs().t() @ x.double().abs()) + 1e-30).all())
