@@ -38,7 +38,7 @@ __device__ __forceinline__ void three_pieces(float v, uint16_t* q) {
     q[0] = piece_of(v);
     const float r1 = v - from_bf16(q[0]);
     const bool finite = fabsf(v) < __builtin_inff();
-    q[1] = finite ? to_bf16(r1) : 0;
+    q[1] = finite ? to_bf16(r1) : 0x7fc0;  // (an infinity: NaN, so that its scores are NaN whatever the signs of the other's pieces)
     q[2] = finite ? to_bf16(r1 - from_bf16(q[1])) : 0;
 }
 

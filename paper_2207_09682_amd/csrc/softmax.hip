@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) void lay_out_fp32_kernel(Fp32Rows w, Fp32Rows 
                 if (finite && b != 0 && b < faint) marked |= RANGE_FAINT;
                 hi.h[k] = to_f16(x);
                 const float r = x - from_f16(hi.h[k]);
-                lo.h[k] = fabsf(x) < __builtin_inff() ? to_f16(r) : 0;
+                lo.h[k] = fabsf(x) < __builtin_inff() ? to_f16(r) : 0x7e00;  // (an infinity: NaN, as in three_pieces())
                 if constexpr (THREE) {
                     uint16_t q[3];
                     three_pieces(value, q);

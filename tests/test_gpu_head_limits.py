@@ -178,3 +178,26 @@ def test_no_piece_of_fp32_values_is_lost(ctx, n, dim, vocab, kind):  # noqa: F81
     perr = 32 * U * (top + 1)[:, None] * (pu * (1 - pu) + 1e-12) + 8 * U * d.abs()
     assert bool(((got[0].cpu().double() - gx).abs() <= perr @ w.double().abs() + 8 * U * (d.abs() @ w.double().abs()) + 1e-30).all())
     assert bool(((got[1].cpu().double() - gw).abs() <= perr.t() @ x.double().abs() + 8 * U * (d.abs().t() @ x.double().abs()) + 1e-30).all())
+
+
+@pytest.mark.parametrize("where", ["x", "weight"])
+@pytest.mark.parametrize("n,dim,vocab", [(16, 72, 300), (60, 64, 500), (200, 100, 700), (100, 192, 3000), (600, 136, 8300), (2100, 264, 2300)])
+def test_infinite_fp32_values_make_scores_that_are_no_numbers(ctx, n, dim, vocab, where):  # noqa: F811
+    """An infinity that meets values of one sign, in all of their pieces: the header says NaN, and not -infinity, which adds nothing."""
+    x, w, t, u = _problem(n, dim, vocab, torch.float32)
+    w[:, 3] = -(1.0 + 2.0 ** -10 + 2.0 ** -20)
+    x[:, 3] = 1.0 + 2.0 ** -10 + 2.0 ** -20
+    base = ctx.softmax_loss(x.cuda(), w.cuda(), t.cuda())[1].cpu()
+    if where == "x":
+        x[7, 3] = float("inf")
+    else:
+        w[11, 3] = float("-inf")
+    for again in (False, True):  # (and where another row asks for more pieces)
+        lse = ctx.softmax_loss(x.cuda(), w.cuda(), t.cuda())[1].cpu()
+        if where == "x":
+            assert bool(torch.isnan(lse[7])) and bool(torch.isfinite(torch.cat([lse[:7], lse[8:]])).all())
+            assert again or torch.equal(torch.cat([lse[:7], lse[8:]]), torch.cat([base[:7], base[8:]]))
+        else:
+            assert bool(torch.isnan(lse).all())
+        x[9] *= 1e-12
+        x[9, 1] = 1.0
