@@ -1077,10 +1077,15 @@ static void gradients(qgbdt_ctx* ctx, const SoftmaxPlan& p, const typename E::T*
         SweepArgs v = {};
         v.dp = p.dp; v.dim = dim; v.terms = terms; v.unit = common; v.slab_ld = p.slab_ld; v.range = range;
         if (grad_x) {
-            v.kept = xp; v.kept16 = x16; v.kept_ld = p.dp; v.kept_piece = n * p.dp; v.n_kept = (int)n; v.swept16 = w16; v.kept_back = x_back; v.swept_back = w_back;
-            v.swept = wp; v.swept_ld = w_ld; v.swept_piece = w_piece; v.n_swept = (int)n_classes;
-            v.splits = p.x_splits; v.out = grad_x; v.slab = p.x_slabs ? reinterpret_cast<float*>(s + p.xs) : nullptr; v.slab_size = n * p.slab_ld;
-            launch_sweep<E, PIECES, SWEEP_ROWS>(ctx, p.sweep, v);
+            v.swept = wp; v.swept_ld = w_ld; v.swept_piece = w_piece; v.n_swept = (int)n_classes; v.swept16 = w16; v.swept_back = w_back;
+            v.kept_ld = p.dp; v.kept_piece = n * p.dp; v.splits = p.x_splits;
+            v.slab = p.x_slabs ? reinterpret_cast<float*>(s + p.xs) : nullptr; v.slab_size = n * p.slab_ld;
+            for (int64_t r0 = 0; r0 < n; r0 += SWEEP_MOST) {  // (so many rows are never in slabs)
+                v.kept = xp + r0 * p.dp; v.kept16 = x16 + r0 * p.dp; v.kept_back = x_back + r0; v.terms = terms + r0; v.out = grad_x + r0 * dim;
+                v.n_kept = (int)(n - r0 < SWEEP_MOST ? n - r0 : SWEEP_MOST);
+                launch_sweep<E, PIECES, SWEEP_ROWS>(ctx, p.sweep, v);
+            }
+            v.terms = terms;
             if (v.slab) join_slabs<E>(ctx, v.slab, v.slab_size, p.slab_ld, p.x_splits, n, dim, grad_x, common);
         }
         if (grad_w) {

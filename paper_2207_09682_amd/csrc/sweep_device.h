@@ -15,6 +15,7 @@ namespace qgbdt {
 enum { SWEEP_STATS, SWEEP_ROWS, SWEEP_CLASSES };
 constexpr int SWEEP_KEPT = 256;   // rows that a workgroup of 8 wavefronts keeps
 constexpr int SWEEP_TILE = 64;    // rows of the other matrix are filled up to a multiple of this
+constexpr int64_t SWEEP_MOST = 1 << 30;  // rows kept by a launch: fewer than 2^32 threads
 
 // A row of x: p = exp2(score * log2(e) + b), its weight in units of the common one, its class or -1.  A row that is left out has
 // b = -infinity and weight 0.
@@ -32,7 +33,7 @@ struct SweepArgs {
     const uint16_t *swept16, *kept16;
     const uint32_t* range;
     const float *kept_back, *swept_back;  // (CLASSES: the swept rows' are in their terms)
-    int n_kept, n_swept, dp;       // dp: values of a row that exist, a multiple of 8
+    int n_kept, n_swept, dp;       // n_kept: at most SWEEP_MOST; dp: values of a row that exist, a multiple of 8
     int tiles, splits;             // workgroups along the kept rows; parts of the swept ones
     const RowTerms* terms;         // of the rows of x, padded to a multiple of SWEEP_TILE
     const float* unit;
@@ -83,7 +84,7 @@ __device__ __forceinline__ void sweep(const SweepArgs& a) {
     const int id = (int)(blockIdx.x & 7) * per + in;  // neighbouring tiles on one XCD
     if (in >= per || id >= total) return;
     const int split = id / a.tiles, kept0 = (id - split * a.tiles) * SWEEP_KEPT + wave * 32;
-    const int steps = (a.n_swept + TILE - 1) / TILE;
+    const int steps = (int)(((int64_t)a.n_swept + TILE - 1) / TILE);
     const int t0 = (int)((int64_t)steps * split / a.splits), t1 = (int)((int64_t)steps * (split + 1) / a.splits);
 
     // the kept rows: lane % 16 of a block of 16, values 32 k + 8 (lane / 16) + 0..7
@@ -155,14 +156,15 @@ __device__ __forceinline__ void sweep(const SweepArgs& a) {
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(o), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(to)) : "m0");
     };
     auto bring = [&](int step, int stage) {  // (beyond the last step: zeros)
-        const int row0 = step * TILE, left = step < t1 ? a.n_swept - row0 : 0;
+        const int64_t row0 = (int64_t)step * TILE;
+        const int left = step < t1 ? (int)(a.n_swept - row0) : 0;
         const uint32_t to = lds + (uint32_t)stage * (STAGE * 2) + (uint32_t)wave * 1024u;
 #pragma unroll
         for (int j = 0; j < ROUNDS; ++j) {
             const int piece = j * 512 / (TILE * CB);
             const uint16_t* base;
-            if (SP::F16 && MODE != SWEEP_STATS && piece < SP::SCORE) base = a.swept16 + (int64_t)piece * a.n_swept * a.dp + (int64_t)row0 * a.dp;
-            else base = a.swept + (int64_t)(piece - (MODE == SWEEP_STATS ? 0 : SP::SECOND_AT)) * a.swept_piece + (int64_t)row0 * a.swept_ld;
+            if (SP::F16 && MODE != SWEEP_STATS && piece < SP::SCORE) base = a.swept16 + (int64_t)piece * a.n_swept * a.dp + row0 * a.dp;
+            else base = a.swept + (int64_t)(piece - (MODE == SWEEP_STATS ? 0 : SP::SECOND_AT)) * a.swept_piece + row0 * a.swept_ld;
             to_lds(base, at_row[j] < left ? off[j] : 0xfffffff0u, to + j * 8192u);
         }
         if constexpr (SP::TERMS)  // (every wavefront the same: all have as many loads in flight)
@@ -347,7 +349,7 @@ __device__ __forceinline__ void sweep(const SweepArgs& a) {
 #pragma unroll
         for (int h = 0; h < TILE / 32; ++h) {
             scores(tile, h);
-            values(tile, h, step * TILE + h * 32);
+            values(tile, h, MODE == SWEEP_CLASSES ? 0 : step * TILE + h * 32);  // (classes; of rows there may be more than fit)
             second(tile, h);
         }
     }

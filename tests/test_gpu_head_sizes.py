@@ -1,0 +1,52 @@
+"""Operators on token tables and class scores at the largest sizes that they accept: counts next to 2^31, launches next to 2^32 threads."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_head import U, ctx  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+MOST = 2 ** 31 - 1
+
+
+@pytest.fixture(autouse=True)
+def room():
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
+def _needs(gigabytes):
+    if torch.cuda.mem_get_info()[0] < gigabytes * 1e9:
+        pytest.skip(f"needs {gigabytes} GB of device memory")
+
+
+def _parts(n):
+    return [(a, min(n, a + 2 ** 28)) for a in range(0, n, 2 ** 28)]
+
+
+def test_softmax_of_as_many_rows_as_there_may_be(ctx):  # noqa: F811
+    _needs(140)
+    n = MOST
+    at = torch.tensor([0, 5, 2 ** 30 - 1, 2 ** 30, 2 ** 30 + 301, n - 200, n - 64, n - 63, n - 2, n - 1], device="cuda")
+    x = torch.zeros(n, 1, dtype=torch.bfloat16, device="cuda")
+    t = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    u = torch.zeros(n, device="cuda")
+    x[at], t[at], u[at] = 1.0, 0, 0.5
+    w = torch.tensor([[0.5], [0.0]], dtype=torch.bfloat16, device="cuda")
+    loss, lse = ctx.softmax_loss(x, w, t)
+    one = math.log(math.exp(0.5) + 1.0)
+    assert bool(((lse[at].double() - one).abs() <= 32 * U).all()) and bool(((loss[at].double() - (one - 0.5)).abs() <= 32 * U).all())
+    lse[at] = math.log(2.0)
+    for a, b in _parts(n):
+        assert float((lse[a:b] - math.log(2.0)).abs().max()) <= 32 * U
+    lse[at] = one
+    del loss
+    gx, gw = ctx.softmax_gradients(x, w, t, lse, u)
+    p = 1.0 / (1.0 + math.exp(-0.5))
+    # D is rounded to bfloat16, and so are the results
+    assert bool(((gx[at, 0].double() - 0.5 * (p - 1.0) * 0.5).abs() <= 0.25 * 2.0 ** -7).all())
+    assert sum(int((gx[a:b] != 0).sum()) for a, b in _parts(n)) == len(at)
+    assert abs(float(gw[0]) - 5.0 * (p - 1.0)) <= 5.0 * 2.0 ** -7 and abs(float(gw[1]) - 5.0 * (1.0 - p)) <= 5.0 * 2.0 ** -7
