@@ -293,10 +293,10 @@ __global__ __launch_bounds__(256) void sort_few_kernel(FromTokens<I> from, int m
 template <class E, bool TINY>
 __device__ __forceinline__ void add_rows(const typename E::T* __restrict__ grad, const uint2* __restrict__ entry, int bag, int dim, int at, int a, int b, float* sum) {
     constexpr int P = E::PER16, U = 8;
-    for (int i = a; i < b; i += U) {
+    for (uint32_t i = a, end = b; i < end; i += U) {  // (unsigned: b may be 2^31 - 1)
         uint32_t r[U];
 #pragma unroll
-        for (int q = 0; q < U; ++q) r[q] = entry[i + q < b ? i + q : b - 1].y;
+        for (int q = 0; q < U; ++q) r[q] = entry[i + q < end ? i + q : end - 1].y;
         Piece<E> v[U];
 #pragma unroll
         for (int q = 0; q < U; ++q) {
@@ -313,7 +313,7 @@ __device__ __forceinline__ void add_rows(const typename E::T* __restrict__ grad,
         for (int k = 0; k < P; ++k) {
             float t[U];
 #pragma unroll
-            for (int q = 0; q < U; ++q) t[q] = i + q < b ? E::get(v[q].v[k]) : 0.0f;
+            for (int q = 0; q < U; ++q) t[q] = i + q < end ? E::get(v[q].v[k]) : 0.0f;
             sum[k] += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
             __builtin_amdgcn_sched_barrier(0);  // (the others stay as they came: 77 registers instead of 106)
         }
@@ -351,25 +351,26 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(const typename E::T* __
     const int sub = threadIdx.x & (lanes - 1), per = 256 / lanes, group = threadIdx.x / lanes;
     const int pd = (dim + 7) / 8 * 8;
     if ((int)blockIdx.x < unit_blocks) {
-        const int64_t u = (int64_t)blockIdx.x * per + group, a0 = u * unit;
-        if (a0 >= m) return;
-        const int a = (int)a0, b = (int)(a0 + unit < m ? a0 + unit : m);
-        const uint32_t k0 = entry[a].x, k1 = entry[b - 1].x;
-        for (int slot = 0; slot < 2; ++slot) {
-            const uint32_t k = slot ? k1 : k0;
-            if (k >= n_vocab || (slot && k1 == k0)) continue;
-            const int2 r = range[k];
-            if (r.y - r.x <= unit) continue;
-            const int from = r.x > a ? r.x : a, to = r.y < b ? r.y : b;
-            for (int c = sub * P; c < dim; c += lanes * P) {
-                const int at = piece_at<E, TINY>(c, dim);
-                float sum[P];
+        for (int64_t u = (int64_t)blockIdx.x * per + group; u * unit < m; u += (int64_t)unit_blocks * per) {
+            const int64_t a0 = u * unit;
+            const int a = (int)a0, b = (int)(a0 + unit < m ? a0 + unit : m);
+            const uint32_t k0 = entry[a].x, k1 = entry[b - 1].x;
+            for (int slot = 0; slot < 2; ++slot) {
+                const uint32_t k = slot ? k1 : k0;
+                if (k >= n_vocab || (slot && k1 == k0)) continue;
+                const int2 r = range[k];
+                if (r.y - r.x <= unit) continue;
+                const int from = r.x > a ? r.x : a, to = r.y < b ? r.y : b;
+                for (int c = sub * P; c < dim; c += lanes * P) {
+                    const int at = piece_at<E, TINY>(c, dim);
+                    float sum[P];
 #pragma unroll
-                for (int q = 0; q < P; ++q) sum[q] = 0.0f;
-                add_rows<E, TINY>(grad, entry, bag, dim, at, from, to, sum);
-                float* const o = part + (u * 2 + slot) * pd + at;
+                    for (int q = 0; q < P; ++q) sum[q] = 0.0f;
+                    add_rows<E, TINY>(grad, entry, bag, dim, at, from, to, sum);
+                    float* const o = part + (u * 2 + slot) * pd + at;
 #pragma unroll
-                for (int q = 0; q < P; q += 4) store_piece<F32>(o + q, sum + q);  // (pd holds a whole piece of a tiny row)
+                    for (int q = 0; q < P; q += 4) store_piece<F32>(o + q, sum + q);  // (pd holds a whole piece of a tiny row)
+                }
             }
         }
         return;
@@ -566,9 +567,10 @@ static void embed_sums(qgbdt_ctx* ctx, const EmbedPlan& p, const uint2* entry, c
     typedef typename E::T T;
     const int lanes = lanes_of_row(dim, E::PER16, p.units), per = 256 / lanes;
     const bool many = p.m > p.unit;
-    const int unit_blocks = many ? (int)((p.units + per - 1) / per) : 0;
+    // (at most 2^22 workgroups of either kind, so that a launch has fewer than 2^32 threads)
+    const int unit_blocks = many ? blocks_for(p.units, per, 1 << 22) : 0;
     int each = 1;
-    while (each < 16 && p.m / per / each > 16384) each *= 2;
+    while ((each < 16 && p.m / per / each > 16384) || p.m / per / each >= 1 << 22) each *= 2;
     const int64_t span = (int64_t)per * each, token_blocks = (p.m + span - 1) / span;
     const int zero_blocks = accumulate ? 0 : blocks_for(n_vocab, per * 4, 4096);
     const int blocks = token_blocks > zero_blocks ? (int)token_blocks : zero_blocks;

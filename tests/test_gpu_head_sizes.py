@@ -50,3 +50,32 @@ def test_softmax_of_as_many_rows_as_there_may_be(ctx):  # noqa: F811
     assert bool(((gx[at, 0].double() - 0.5 * (p - 1.0) * 0.5).abs() <= 0.25 * 2.0 ** -7).all())
     assert sum(int((gx[a:b] != 0).sum()) for a, b in _parts(n)) == len(at)
     assert abs(float(gw[0]) - 5.0 * (p - 1.0)) <= 5.0 * 2.0 ** -7 and abs(float(gw[1]) - 5.0 * (1.0 - p)) <= 5.0 * 2.0 ** -7
+
+
+def test_lookup_gradient_of_as_many_tokens_as_there_may_be(ctx):  # noqa: F811
+    """One token in all places but a few: its entries end with the last one, 2^31 - 1."""
+    _needs(80)
+    n = MOST
+    t = torch.ones(n, dtype=torch.int32, device="cuda")
+    grad = torch.zeros(n, 1, dtype=torch.bfloat16, device="cuda")
+    t[3], t[n - 9], grad[3], grad[n - 9] = 0, 0, 3.0, 4.0
+    at = torch.tensor([0, 1, 17, 2 ** 30, 2 ** 31 - 70, n - 8, n - 7, n - 2, n - 1], device="cuda")
+    grad[at] = 1.0
+    got = ctx.embed_gradient(t, grad, 3)
+    assert got[:, 0].tolist() == [7.0, 9.0, 0.0]
+
+
+def test_lookup_gradient_of_many_entries_of_wide_rows(ctx):  # noqa: F811
+    """A workgroup per token and sixteen entries of each would be 2^32 threads: few rows of 1024 values in very large bags."""
+    _needs(20)
+    n, bag, dim, vocab = 4200, 65536, 1024, 4096
+    t = torch.randint(0, vocab, (n, bag), dtype=torch.int32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    grad = (torch.arange(n, device="cuda") % 8 == 0).float()[:, None] * (1.0 + torch.arange(dim, device="cuda").float()[None]) / 1024.0
+    counts = torch.zeros(n, vocab, dtype=torch.float64, device="cuda")
+    for a in range(0, n, 300):
+        rows = t[a:a + 300].long()
+        counts[a:a + 300].scatter_add_(1, rows, torch.ones(rows.shape, dtype=torch.float64, device="cuda"))
+    got = ctx.embed_gradient(t, grad, vocab + 1)
+    want = counts.t().contiguous() @ grad.double()
+    assert bool(((got[:vocab].double() - want).abs() <= 33 * U * want).all())
+    assert bool((got[vocab] == 0).all())
