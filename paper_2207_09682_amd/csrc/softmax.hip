@@ -720,7 +720,8 @@ static void launch_middle(qgbdt_ctx* ctx, MiddleArgs a, const Epilogue& e, int64
     else pick(std::false_type());
 }
 
-constexpr int64_t ROW_BLOCK = 131072;       // rows whose gradients are taken together
+constexpr int64_t ROW_BLOCK = 131072;       // rows whose scores, or gradients, are taken together
+constexpr int64_t BLOCK_SCORES = 1ll << 37; // scores of such a block in the loss: 8 GB of maxima and sums, 2^21 tiles of the largest kind, 2^30 threads
 constexpr int64_t D_VALUES = 128ll << 20;   // values of D that are kept at a time
 
 // Whether the rows are short enough to be swept (sweep_device.h), and to how many values they are filled up; 0: not.
@@ -799,7 +800,9 @@ static SoftmaxPlan make_softmax_plan(int64_t n, int dim, int64_t n_classes, int 
     }
     // (the loss reads no other pieces than those)
     p.w = p.copy_w && (gradients || !halves) ? take((size_t)n_classes * p.dp * 2 * p.pieces) : 0;
-    p.row_block = n < ROW_BLOCK ? n : ROW_BLOCK;
+    p.row_block = ROW_BLOCK;
+    while (!gradients && p.row_block * n_classes > BLOCK_SCORES) p.row_block /= 2;
+    if (p.row_block > n) p.row_block = n;
     p.row_blocks = n > 0 ? (n + p.row_block - 1) / p.row_block : 0;
     if (!gradients) {
         if (halves) {

@@ -79,3 +79,25 @@ def test_lookup_gradient_of_many_entries_of_wide_rows(ctx):  # noqa: F811
     want = counts.t().contiguous() @ grad.double()
     assert bool(((got[:vocab].double() - want).abs() <= 33 * U * want).all())
     assert bool((got[vocab] == 0).all())
+
+
+def test_loss_of_many_rows_against_millions_of_classes(ctx):  # noqa: F811
+    """131,072 rows at once against so many classes would be 2^32 threads of the largest tiles: the rows are taken in smaller blocks."""
+    _needs(30)
+    n, dim, vocab = 131_072 + 5, 264, 4_400_003
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w = torch.randn(vocab, dim, generator=g, device="cuda", dtype=torch.bfloat16) * 0.06
+    t = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+    x = torch.randn(n, dim, generator=g, device="cuda", dtype=torch.bfloat16)
+    loss, lse = ctx.softmax_loss(x, w, t)
+    at = torch.tensor([0, 1, 16383, 16384, 32767, 32768, 65535, 65536, 131_071, 131_072, n - 1], device="cuda")
+    want = torch.full((len(at),), -math.inf, dtype=torch.float64, device="cuda")
+    mag = torch.zeros(len(at), dtype=torch.float64, device="cuda")
+    for a in range(0, vocab, 200_000):
+        ws = w[a:a + 200_000].double()
+        want = torch.logaddexp(want, torch.logsumexp(x[at].double() @ ws.t(), 1))
+        mag = torch.maximum(mag, (x[at].double().abs() @ ws.abs().t()).amax(1))
+    score = (x[at].double() * w[t[at]].double()).sum(1)
+    assert bool(((lse[at].double() - want).abs() <= 32 * U * (1 + mag + want.abs())).all())
+    assert bool(((loss[at].double() - (want - score)).abs() <= 64 * U * (1 + mag + want.abs())).all())
+    assert bool(torch.isfinite(loss).all())
