@@ -38,7 +38,10 @@ __device__ __forceinline__ void put_piece(typename E::T* p, int dim, const float
 // A group of `lanes` threads per row; BAG rows of a bag are requested at a time (1: a plain lookup, then two rows are in flight).  Bound by
 // memory (16,384 x 2048 bf16: 16.5 us, 5.8 TB/s), with short rows by the requests to the caches (5.2 M rows of 256 bytes: 102 us, 13 TB/s of which
 // 5.5 come from memory).
-template <class E, class I, bool TINY, int BAG>
+//
+// LONG: bags of more than 64 rows, whose sums would lose more with every row (65,536 equal values: up to 14,000 units of 2^-24), keep what the
+// additions lose.  In shorter ones that would cost registers and, where rows come from the caches, time (5000 bags of 26 x 512 fp16: 16.1 us, with it 17.8).
+template <class E, class I, bool TINY, int BAG, bool LONG>
 __global__ __launch_bounds__(256) void embed_kernel(const typename E::T* __restrict__ table, int64_t n_vocab, int dim, int64_t stride,
                                                     const void* __restrict__ tokens, int64_t n, int bag, float scale,
                                                     typename E::T* __restrict__ out, int lanes) {
@@ -48,11 +51,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const typename E::T* __restr
     for (int64_t i = (int64_t)blockIdx.x * per + threadIdx.x / lanes; i < n; i += groups * ROWS)
         for (int c = sub * P; c < dim; c += lanes * P) {
             const int at = piece_at<E, TINY>(c, dim);
-            float sum[ROWS][P];
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-                for (int k = 0; k < P; ++k) sum[r][k] = 0.0f;
+            LongSum sum[ROWS][P];
             for (int b = 0; b < bag; b += BAG) {
                 // (no token, padding: row 0 is read and not used)
                 bool on[ROWS * BAG];
@@ -66,16 +65,29 @@ __global__ __launch_bounds__(256) void embed_kernel(const typename E::T* __restr
                     on[q] = t >= 0 && t < n_vocab;
                     get_piece<E, TINY>(table + (on[q] ? t : 0) * stride + at, dim, v[q]);
                 }
+                float part[ROWS][P];
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                    for (int k = 0; k < P; ++k) part[r][k] = LONG ? 0.0f : sum[r][k].sum;
 #pragma unroll
                 for (int q = 0; q < ROWS * BAG; ++q)
 #pragma unroll
-                    for (int k = 0; k < P; ++k) sum[ROWS > 1 ? q : 0][k] += on[q] ? v[q][k] : 0.0f;
+                    for (int k = 0; k < P; ++k) part[ROWS > 1 ? q : 0][k] += on[q] ? v[q][k] : 0.0f;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                    for (int k = 0; k < P; ++k) {
+                        if constexpr (LONG) sum[r][k].add(part[r][k]);
+                        else sum[r][k].sum = part[r][k];
+                    }
             }
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
+                float o[P];
 #pragma unroll
-                for (int k = 0; k < P; ++k) sum[r][k] *= scale;
-                if (r == 0 || i + r * groups < n) put_piece<E, TINY>(out + (i + r * groups) * dim + at, dim, sum[r]);
+                for (int k = 0; k < P; ++k) o[k] = (LONG ? sum[r][k].value() : sum[r][k].sum) * scale;
+                if (r == 0 || i + r * groups < n) put_piece<E, TINY>(out + (i + r * groups) * dim + at, dim, o);
             }
         }
 }
@@ -529,9 +541,11 @@ static void embed_tokens(qgbdt_ctx* ctx, const void* table, int64_t n_vocab, int
     const dim3 grid(blocks_for(n, 256 / lanes * (bag == 1 ? 2 : 1), 1 << 20)), threads(256);
     const typename E::T* const t = static_cast<const typename E::T*>(table);
     typename E::T* const o = static_cast<typename E::T*>(out);
-    if (dim < E::PER16) hipLaunchKernelGGL((embed_kernel<E, I, true, 4>), grid, threads, 0, ctx->stream, t, n_vocab, dim, stride, tokens, n, bag, scale, o, lanes);
-    else if (bag == 1) hipLaunchKernelGGL((embed_kernel<E, I, false, 1>), grid, threads, 0, ctx->stream, t, n_vocab, dim, stride, tokens, n, bag, scale, o, lanes);
-    else hipLaunchKernelGGL((embed_kernel<E, I, false, 8>), grid, threads, 0, ctx->stream, t, n_vocab, dim, stride, tokens, n, bag, scale, o, lanes);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, ctx->stream, t, n_vocab, dim, stride, tokens, n, bag, scale, o, lanes); };
+    const bool longer = bag > 64;
+    if (dim < E::PER16) longer ? go(embed_kernel<E, I, true, 4, true>) : go(embed_kernel<E, I, true, 4, false>);
+    else if (bag == 1) go(embed_kernel<E, I, false, 1, false>);
+    else longer ? go(embed_kernel<E, I, false, 8, true>) : go(embed_kernel<E, I, false, 8, false>);
 }
 
 int run_embed_tokens(qgbdt_ctx* ctx, const void* table, int dtype, int64_t n_vocab, int dim, int64_t table_stride, const void* tokens, int token_bytes, int64_t n,

@@ -66,6 +66,18 @@ __device__ __forceinline__ void store_part(typename E::T* p, int m, const float*
         if (i < m) p[i] = E::put(v[i]);
 }
 
+// A sum that keeps what its roundings lose (the exact error of an addition of two floats, after Knuth), so that its own error does not grow with its length.
+// An infinite sum stays one.
+struct LongSum {
+    float sum = 0.0f, lost = 0.0f;
+    __device__ __forceinline__ void add(float v) {
+        const float s = sum + v, b = s - sum;
+        lost += (sum - (s - b)) + (v - b);
+        sum = s;
+    }
+    __device__ __forceinline__ float value() const { return fabsf(sum) < __builtin_inff() ? sum + lost : sum; }
+};
+
 // LDS writes of a wavefront's lanes are there for its other lanes
 __device__ __forceinline__ void wavefront_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

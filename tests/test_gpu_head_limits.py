@@ -201,3 +201,33 @@ def test_infinite_fp32_values_make_scores_that_are_no_numbers(ctx, n, dim, vocab
             assert bool(torch.isnan(lse).all())
         x[9] *= 1e-12
         x[9, 1] = 1.0
+
+
+# ---- long sums -----------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n,bag,dim,vocab", [(3, 60_000, 12, 500), (2, 65_536, 33, 1), (5, 40_001, 3, 2), (70, 3001, 260, 3)])
+def test_lookup_of_long_bags(ctx, dtype, n, bag, dim, vocab):  # noqa: F811
+    """Few distinct values, added up tens of thousands of times: the roundings of a sum of one after the other would all go one way.  Sums of eight and a sum of these
+    that keeps its roundings are off by 5 u; the bound is 8 u of the sum of magnitudes and the rounding to the type."""
+    g = _gen(bag)
+    table = (1.0 + torch.rand(vocab, dim, generator=g)).to(dtype)
+    tok = torch.randint(0, vocab, (n, bag), generator=g)
+    tok[:, 5] = -1
+    scale = 2.0 ** -17  # (in fp16 the sums themselves are beyond the type)
+    want = torch.stack([(table.double()[tok[i].clamp(min=0)] * (tok[i] >= 0)[:, None]).sum(0) * scale for i in range(n)])
+    r = ROUND[dtype] + 8 * U
+    for t in (tok, tok.int()):
+        got = ctx.embed_tokens(table.cuda(), t.cuda(), scale).cpu().double()
+        assert bool(((got - want).abs() <= r * want).all()), float(((got - want).abs() / want).max() / U)
+
+
+def test_lookup_of_bags_with_infinite_rows(ctx):  # noqa: F811
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        table = torch.ones(4, 9).to(dtype)
+        table[1], table[2], table[3] = float("inf"), float("-inf"), float("nan")
+        tok = torch.zeros(4, 50, dtype=torch.int32)
+        tok[0, 3], tok[1, 30], tok[2, 4], tok[2, 40], tok[3, 20] = 1, 2, 1, 2, 3
+        got = ctx.embed_tokens(table.cuda(), tok.cuda()).cpu().float()
+        assert bool((got[0] == math.inf).all()) and bool((got[1] == -math.inf).all()) and bool(torch.isnan(got[2:]).all())
