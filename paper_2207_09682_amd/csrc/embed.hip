@@ -459,9 +459,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void embed_merge_kernel(const uint2*
         const int64_t last = (r.y - 1) / unit;
         for (int c0 = 0; c0 < dim; c0 += lanes * P) {
             const int c = c0 + sub * P;
-            float sum[P];
-#pragma unroll
-            for (int q = 0; q < P; ++q) sum[q] = 0.0f;
+            LongSum parts[P];  // (a token of all of 2^31 entries has 33 million parts)
             if (c < dim)
                 for (int64_t w0 = u + group; w0 <= last; w0 += 4 * per) {
                     float v[4][P];
@@ -476,8 +474,11 @@ __global__ __launch_bounds__(MERGE_THREADS) void embed_merge_kernel(const uint2*
                         for (int q = 0; q < P; q += 4) load_piece<F32>(p + q, v[h] + q);
                     }
 #pragma unroll
-                    for (int q = 0; q < P; ++q) sum[q] += (v[0][q] + v[1][q]) + (v[2][q] + v[3][q]);
+                    for (int q = 0; q < P; ++q) parts[q].add((v[0][q] + v[1][q]) + (v[2][q] + v[3][q]));
                 }
+            float sum[P];
+#pragma unroll
+            for (int q = 0; q < P; ++q) sum[q] = parts[q].value();
             for (int half = per >> 1; half > 0; half >>= 1) {  // the groups' sums, as a tree
                 __syncthreads();
 #pragma unroll

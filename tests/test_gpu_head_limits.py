@@ -231,3 +231,24 @@ def test_lookup_of_bags_with_infinite_rows(ctx):  # noqa: F811
         tok[0, 3], tok[1, 30], tok[2, 4], tok[2, 40], tok[3, 20] = 1, 2, 1, 2, 3
         got = ctx.embed_tokens(table.cuda(), tok.cuda()).cpu().float()
         assert bool((got[0] == math.inf).all()) and bool((got[1] == -math.inf).all()) and bool(torch.isnan(got[2:]).all())
+
+
+@pytest.mark.parametrize("n,dim,vocab", [(2_000_003, 1024, 2), (4_000_003, 5, 1), (700_001, 264, 3)])
+def test_lookup_gradient_of_very_frequent_tokens(ctx, n, dim, vocab):  # noqa: F811
+    """Hundreds of thousands of rows of few distinct values per token, of one sign: units of 64 as trees of eight (11 u), four units at a time and a sum of these that keeps
+    its roundings (5 u)."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    tok = torch.randint(0, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
+    kinds = (1.0 + torch.rand(7, dim, generator=g, device="cuda")).bfloat16()
+    pick = torch.randint(0, 7, (n,), generator=g, device="cuda")
+    grad = kinds[pick]
+    got = ctx.embed_gradient(tok, grad, vocab, 2.0 ** -20)
+    counts = torch.zeros(vocab, 7, dtype=torch.float64, device="cuda")
+    counts.view(-1).scatter_add_(0, tok.long() * 7 + pick, torch.ones(n, dtype=torch.float64, device="cuda"))
+    want = counts @ kinds.double() * 2.0 ** -20
+    assert bool(((got.double() - want).abs() <= (2.0 ** -8 + 16 * U) * want).all())
+    full = ctx.embed_gradient(tok[:400_000], grad[:400_000].float(), vocab, 2.0 ** -20)
+    counts = torch.zeros(vocab, 7, dtype=torch.float64, device="cuda")
+    counts.view(-1).scatter_add_(0, tok[:400_000].long() * 7 + pick[:400_000], torch.ones(400_000, dtype=torch.float64, device="cuda"))
+    want = counts @ kinds.double() * 2.0 ** -20
+    assert bool(((full.double() - want).abs() <= 17 * U * want).all()), float(((full.double() - want).abs() / want).max() / U)
