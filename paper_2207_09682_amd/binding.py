@@ -293,7 +293,9 @@ class Context:
             raise RuntimeError("no GPU: the qgbdt library runs on MI355X only (no CPU path)")
         self.lib = load_library()
         self.device = torch.device(device)
-        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        if self.device.index is None:  # (the device of now: what the context allocates later belongs on it too)
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.shape = Shape(n_rows, n_features, n_bins, bin_bytes, max_leaves)
         self._h = C.c_void_p()
         with torch.cuda.device(self.device):
@@ -534,6 +536,7 @@ class Context:
             scratch = torch.empty(max(need.value, 1), dtype=torch.uint8, device=self.device)
         else:
             _dev(scratch, torch.uint8, "scratch")
+            self._here(scratch)
         return scratch, scratch.numel()
 
     def embed_tokens(self, table, tokens, scale=1.0, out=None):
@@ -639,6 +642,10 @@ class Context:
         scratch, room = self._scratch(scratch, self.lib.qgbdt_clip_gradients_bytes, n)
         if norm is None:
             norm = torch.empty(1, dtype=torch.float32, device=self.device)
+        elif norm.numel() < 1:
+            raise ValueError("norm must hold a value")
+        else:
+            self._here(norm)
         src, dst = array("Q", map(address, tensors)), array("Q", map(address, out))
         self._chk(self.lib.qgbdt_clip_gradients(self._h, src.buffer_info()[0], dst.buffer_info()[0], counts.buffer_info()[0],
                                                 codes.buffer_info()[0], n, float(max_norm), _dev(norm, torch.float32, "norm"), scratch.data_ptr(), room))

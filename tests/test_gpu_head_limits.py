@@ -252,3 +252,26 @@ def test_lookup_gradient_of_very_frequent_tokens(ctx, n, dim, vocab):  # noqa: F
     counts.view(-1).scatter_add_(0, tok[:400_000].long() * 7 + pick[:400_000], torch.ones(400_000, dtype=torch.float64, device="cuda"))
     want = counts @ kinds.double() * 2.0 ** -20
     assert bool(((full.double() - want).abs() <= 17 * U * want).all()), float(((full.double() - want).abs() / want).max() / U)
+
+
+# ---- where blocks and results lie ------------------------------------------------------------------------
+
+
+def test_blocks_of_another_device_are_refused():
+    """The context's number is changed instead of the tensors' device: a second card is not needed."""
+    from paper_2207_09682_amd import Context
+    c = Context(1, 1, 2, max_leaves=1, workspace_flags=0, device="cuda")
+    assert c.device == torch.device("cuda", torch.cuda.current_device())
+    scratch, norm = torch.empty(1 << 16, dtype=torch.uint8, device=c.device), torch.zeros(1, device=c.device)
+    with pytest.raises(ValueError):
+        c.clip_gradients([], 1.0, norm=torch.zeros(0, device=c.device))
+    assert float(c.clip_gradients([], 1.0, norm=norm, scratch=scratch)) == 0.0
+    stream = c._sync_stream
+    c._index, c._sync_stream = c._index + 1, lambda: None
+    try:
+        with pytest.raises(ValueError):
+            c.clip_gradients([], 1.0, scratch=scratch)
+        with pytest.raises(ValueError):
+            c.clip_gradients([], 1.0, norm=norm)
+    finally:
+        c._index, c._sync_stream = c._index - 1, stream
