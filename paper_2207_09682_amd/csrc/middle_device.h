@@ -74,7 +74,6 @@ __global__ __launch_bounds__(64 * WL * WR) void middle_kernel(MiddleArgs a, Epil
     FragReader<BL, false> fl;
     fl.init(wl * (BL / WL), lane);
     constexpr int LOADS_L = TileLoader<BL, T, false>::ROUNDS, LOADS = 3 * LOADS_L + WeightLoader<BR, T, TR, WIDE>::ROUNDS;
-    static_assert(BL * PK / 8 >= T, "every wavefront has a part in a piece's load");
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)product_tiles;
     int next = t0;
     auto load = [&](int stage) {  // (beyond the last step: zeros, so that the loads in flight are always as many)
@@ -85,7 +84,7 @@ __global__ __launch_bounds__(64 * WL * WR) void middle_kernel(MiddleArgs a, Epil
         for (int p = 0; p < 3; ++p) {
             ll.seek(next, p);
 #pragma unroll
-            for (int j = 0; j < LOADS_L; ++j) ll.load(j, to + p * L * 2, 0, wave, next, next < t1);
+            for (int j = 0; j < LOADS_L; ++j) ll.load(j, to + p * L * 2, wave, next, next < t1);
         }
         lw.base += lw.advance;
         ++next;

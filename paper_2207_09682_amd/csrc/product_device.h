@@ -78,7 +78,8 @@ template <int B, int T, bool TR>
 struct TileLoader {
     static constexpr int CB = B / 8;
     static constexpr int PIECES = B * PK / 8;                       // of 16 bytes
-    static constexpr int ROUNDS = PIECES > T ? PIECES / T : 1;      // (fewer pieces than threads: the last wavefronts' go to a spare place)
+    static constexpr int ROUNDS = PIECES / T;
+    static_assert(PIECES % T == 0 && PIECES >= T, "every wavefront has a part in every round");
     static constexpr int PER_ROUND = TR ? T / CB : T / (PK / 8);    // rows (of k when transposed) per round
     uint32_t off[ROUNDS];  // bytes from the base
     const uint16_t* base;  // of the next step
@@ -113,16 +114,14 @@ struct TileLoader {
     }
     __device__ __forceinline__ void seek(int step, int pc) { base = start + (int64_t)pc * piece + step * advance; }
 
-    // Round j of a step's loads.  lds: byte address of the tile; spare: of 1 KB per wavefront beyond the pieces
-    __device__ __forceinline__ void load(int j, uint32_t lds, uint32_t spare, int wave, int step, bool more) const {
+    // Round j of a step's loads.  lds: byte address of the tile
+    __device__ __forceinline__ void load(int j, uint32_t lds, int wave, int step, bool more) const {
         typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
         const uint64_t at = (uint64_t)base;
         const u32x4 rsrc = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
         const int left = (more ? k : -(1 << 30)) - step * PK - kk;
         const uint32_t o = left > (TR ? j * PER_ROUND : 0) ? off[j] : 0xfffffff0u;
-        uint32_t to = lds + (uint32_t)(j * T + wave * 64) * 16u;
-        if (PIECES < T && wave * 64 >= PIECES) to = spare + (uint32_t)(wave - PIECES / 64) * 1024u;
-        to = __builtin_amdgcn_readfirstlane(to);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (uint32_t)(j * T + wave * 64) * 16u);
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(o), "s"(rsrc), "s"(to) : "m0");
     }
 };
@@ -151,10 +150,7 @@ struct FragReader {
     }
 };
 
-// bytes of LDS: the stages, and room for loads of wavefronts that have no part in a small tile
-__host__ __device__ constexpr int product_lds(int bl, int br, int threads, int stages) {
-    return stages * (bl + br) * PK * 2 + ((bl < br ? bl : br) * PK / 8 < threads ? threads * 16 : 0);
-}
+__host__ __device__ constexpr int product_lds(int bl, int br, int stages) { return stages * (bl + br) * PK * 2; }  // bytes
 
 // WL x WR wavefronts, each with (BL / WL) x (BR / WR) values of C.  A step is 64 values of k, two halves of 32, and STAGES steps are in
 // LDS or on their way.  Early in the second half of step t, whose operands are in registers by then, the wavefronts meet: everybody
@@ -211,14 +207,14 @@ __device__ __forceinline__ void product_sums(const ProductArgs& a, const Product
         lr.seek(step, (a.pieces_r >> (4 * seg)) & 0xf);
     };
     seek();
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)product_tiles, spare = lds + STAGES * STAGE * 2;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)product_tiles;
     int into = 0;  // stage of the next load
     constexpr int LOADS_L = TileLoader<BL, T, LT>::ROUNDS, LOADS = LOADS_L + TileLoader<BR, T, RT>::ROUNDS;  // of a step
     // load i of step `next` (beyond the last step: zeros, so that the loads in flight are always as many)
     auto load = [&](int i) {
         const uint32_t to = lds + (uint32_t)into * (STAGE * 2);
-        if (i < LOADS_L) ll.load(i, to, spare, wave, step, next < t1);
-        else lr.load(i - LOADS_L, to + BL * PK * 2, spare, wave, step, next < t1);
+        if (i < LOADS_L) ll.load(i, to, wave, step, next < t1);
+        else lr.load(i - LOADS_L, to + BL * PK * 2, wave, step, next < t1);
     };
     auto loaded = [&]() {
         into = into + 1 == STAGES ? 0 : into + 1;

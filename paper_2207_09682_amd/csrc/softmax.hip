@@ -630,11 +630,11 @@ static void launch_product(qgbdt_ctx* ctx, int tile, ProductArgs a, const Epilog
         allow_lds(ctx, reinterpret_cast<const void*>(kernel), lds);
         hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, ctx->stream, a, e);
     };
-    if (tile == TILE_256) go(product_kernel<256, 256, 4, 2, 2, LT, RT, Epilogue>, 512, product_lds(256, 256, 512, 2));
-    else if (tile == TILE_128) go(product_kernel<128, 128, 2, 2, 2, LT, RT, Epilogue>, 256, product_lds(128, 128, 256, 2));
-    else if (tile == TILE_128x64) go(product_kernel<128, 64, 4, 1, 3, LT, RT, Epilogue>, 256, product_lds(128, 64, 256, 3));
-    else if (tile == TILE_64) go(product_kernel<64, 64, 2, 2, 3, LT, RT, Epilogue>, 256, product_lds(64, 64, 256, 3));
-    else if constexpr (!Epilogue::TURNS) go(product_kernel<32, 128, 1, 4, 6, LT, RT, Epilogue>, 256, product_lds(32, 128, 256, 6));  // (D has 64 rows at least)
+    if (tile == TILE_256) go(product_kernel<256, 256, 4, 2, 2, LT, RT, Epilogue>, 512, product_lds(256, 256, 2));
+    else if (tile == TILE_128) go(product_kernel<128, 128, 2, 2, 2, LT, RT, Epilogue>, 256, product_lds(128, 128, 2));
+    else if (tile == TILE_128x64) go(product_kernel<128, 64, 4, 1, 3, LT, RT, Epilogue>, 256, product_lds(128, 64, 3));
+    else if (tile == TILE_64) go(product_kernel<64, 64, 2, 2, 3, LT, RT, Epilogue>, 256, product_lds(64, 64, 3));
+    else if constexpr (!Epilogue::TURNS) go(product_kernel<32, 128, 1, 4, 6, LT, RT, Epilogue>, 256, product_lds(32, 128, 6));  // (D has 64 rows at least)
 }
 
 // Scores of fp32 rows; `three`: where their three bfloat16 pieces lie, of x and of the weights.
@@ -648,11 +648,11 @@ static void launch_scores(qgbdt_ctx* ctx, int tile, ProductArgs a, const uint16_
         allow_lds(ctx, reinterpret_cast<const void*>(kernel), lds);
         hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, ctx->stream, a, b, range, e);
     };
-    if (tile == TILE_256) go(score_kernel<256, 256, 4, 2, 2, Epilogue>, 512, product_lds(256, 256, 512, 2));
-    else if (tile == TILE_128) go(score_kernel<128, 128, 2, 2, 2, Epilogue>, 256, product_lds(128, 128, 256, 2));
-    else if (tile == TILE_128x64) go(score_kernel<128, 64, 4, 1, 3, Epilogue>, 256, product_lds(128, 64, 256, 3));
-    else if (tile == TILE_64) go(score_kernel<64, 64, 2, 2, 3, Epilogue>, 256, product_lds(64, 64, 256, 3));
-    else if constexpr (!Epilogue::TURNS) go(score_kernel<32, 128, 1, 4, 6, Epilogue>, 256, product_lds(32, 128, 256, 6));
+    if (tile == TILE_256) go(score_kernel<256, 256, 4, 2, 2, Epilogue>, 512, product_lds(256, 256, 2));
+    else if (tile == TILE_128) go(score_kernel<128, 128, 2, 2, 2, Epilogue>, 256, product_lds(128, 128, 2));
+    else if (tile == TILE_128x64) go(score_kernel<128, 64, 4, 1, 3, Epilogue>, 256, product_lds(128, 64, 3));
+    else if (tile == TILE_64) go(score_kernel<64, 64, 2, 2, 3, Epilogue>, 256, product_lds(64, 64, 3));
+    else if constexpr (!Epilogue::TURNS) go(score_kernel<32, 128, 1, 4, 6, Epilogue>, 256, product_lds(32, 128, 6));
 }
 
 // Whether the products read fp32 weights where they lie (middle_device.h).  Scores of pieces that are made once take half the products: the loss of
@@ -1162,7 +1162,7 @@ static void gradients(qgbdt_ctx* ctx, const SoftmaxPlan& p, const typename E::T*
             if (p.middle) {
                 if (grad_w) launch_product<true, true>(ctx, tw, aw, ew, cols, dim);
             } else if (grad_x && grad_w && bx + bw <= 1024 && (int64_t)ax.steps * ax.segs <= 16 * ax.splits && (int64_t)aw.steps * aw.segs <= 16 * aw.splits) {
-                hipLaunchKernelGGL((product_pair_kernel<64, 64, 2, 2, 3, false, true, true, true, StoreEpilogue<E>>), dim3(bx + bw), dim3(256), product_lds(64, 64, 256, 3),
+                hipLaunchKernelGGL((product_pair_kernel<64, 64, 2, 2, 3, false, true, true, true, StoreEpilogue<E>>), dim3(bx + bw), dim3(256), product_lds(64, 64, 3),
                                    ctx->stream, sx, ex, sw, ew, (int)bx);
             } else {
                 if (grad_x) launch_product<false, true>(ctx, tx, ax, ex, rows, dim);
