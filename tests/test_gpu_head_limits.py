@@ -275,3 +275,86 @@ def test_blocks_of_another_device_are_refused():
             c.clip_gradients([], 1.0, norm=norm)
     finally:
         c._index, c._sync_stream = c._index - 1, stream
+
+
+# ---- every kernel family: rows that hold anything, streams, graphs ----------------------------------------
+
+# few rows; few rows against few classes; swept; weights where they lie, in tiles of 32, 64 and 128 rows; both second products at once; tiles, an odd number of rows; blocks of rows
+FAMILIES = [(torch.bfloat16, 9, 264, 3000), (torch.bfloat16, 16, 2048, 26_000), (torch.bfloat16, 200, 250, 700), (torch.bfloat16, 33, 300, 200), (torch.bfloat16, 301, 520, 1000),
+            (torch.bfloat16, 2101, 264, 2300), (torch.float32, 3, 40, 500), (torch.float32, 15, 770, 12_500), (torch.float32, 200, 100, 700), (torch.float32, 20, 192, 3000),
+            (torch.float32, 64, 260, 9000), (torch.float32, 120, 1000, 12_000), (torch.float32, 701, 300, 1200), (torch.float32, 2101, 264, 2300)]
+
+
+@pytest.mark.parametrize("dtype,n,dim,vocab", FAMILIES)
+def test_left_out_rows_may_hold_anything_in_every_family(ctx, dtype, n, dim, vocab):  # noqa: F811
+    """Rows without target hold NaN, rows of weight 0 infinities: the other rows' results and the class weights' gradient are the same bits; a live row of NaN poisons its own
+    row and the class weights' gradient, and no other row."""
+    x, w, t, u = _problem(n, dim, vocab, dtype)
+    t[0], t[1], u[2], t[2], u[n - 1], t[n - 1] = 1, -1, 0.0, 3, 1.0, 2  # (the last row counts: rows behind it are read as it)
+    u[0] = 0.5
+    ok = (t >= 0) & (t < vocab)
+    live = ok & (u != 0)
+    loss, lse = ctx.softmax_loss(x.cuda(), w.cuda(), t.cuda())
+    want = ctx.softmax_gradients(x.cuda(), w.cuda(), t.cuda(), lse, u.cuda())
+    bad = x.clone()
+    bad[~ok], bad[ok & (u == 0)] = float("nan"), float("inf")
+    loss2, lse2 = ctx.softmax_loss(bad.cuda(), w.cuda(), t.cuda())
+    assert torch.equal(lse2.cpu()[live], lse.cpu()[live]) and torch.equal(loss2.cpu()[live], loss.cpu()[live]) and bool((loss2.cpu()[~ok] == 0).all())
+    got = ctx.softmax_gradients(bad.cuda(), w.cuda(), t.cuda(), lse2, u.cuda())
+    assert torch.equal(got[0].cpu()[live], want[0].cpu()[live]) and bool((got[0].cpu()[~live] == 0).all()) and torch.equal(got[1], want[1])
+    for row in (0, n - 1):
+        bad = x.clone()
+        bad[row] = float("nan")
+        keep = torch.arange(n) != row
+        loss2, lse2 = ctx.softmax_loss(bad.cuda(), w.cuda(), t.cuda())
+        assert bool(torch.isnan(lse2[row])) and torch.equal(lse2.cpu()[keep], lse.cpu()[keep]) and torch.equal(loss2.cpu()[keep], loss.cpu()[keep])
+        got = ctx.softmax_gradients(bad.cuda(), w.cuda(), t.cuda(), lse2, u.cuda())
+        assert bool(torch.isnan(got[0][row]).all()) and torch.equal(got[0].cpu()[keep], want[0].cpu()[keep]) and bool(torch.isnan(got[1]).all())
+
+
+@pytest.mark.parametrize("dtype,n,dim,vocab", FAMILIES)
+def test_rows_that_lie_apart_in_every_family(ctx, dtype, n, dim, vocab):  # noqa: F811
+    x, w, t, u = _problem(n, dim, vocab, dtype)
+    xs, ws = torch.full((n, dim + 11), float("nan"), dtype=dtype), torch.full((vocab, dim + 5), float("nan"), dtype=dtype)
+    xs[:, :dim], ws[:, :dim] = x, w
+    args, apart = (x.cuda(), w.cuda(), t.cuda()), (xs.cuda()[:, :dim], ws.cuda()[:, :dim], t.cuda())
+    want, got = ctx.softmax_loss(*args), ctx.softmax_loss(*apart)
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+    a, b = ctx.softmax_gradients(*args, want[1], u.cuda()), ctx.softmax_gradients(*apart, want[1], u.cuda())
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype,n,dim,vocab", FAMILIES)
+def test_graphs_and_streams_in_every_family(ctx, dtype, n, dim, vocab):  # noqa: F811
+    x, w, t, u = (a.cuda() for a in _problem(n, dim, vocab, dtype))
+    e = lambda *s, d=dtype: torch.zeros(s, dtype=d, device="cuda")  # noqa: E731
+    room = lambda: (e(n, d=torch.float32), e(n, d=torch.float32), e(n, dim), e(vocab, dim))  # noqa: E731
+
+    def step(o):
+        loss, lse = ctx.softmax_loss(x, w, t, loss=o[0], lse=o[1])
+        ctx.softmax_gradients(x, w, t, lse, u, grad_x=o[2], grad_weight=o[3])
+
+    want, other, rec = room(), room(), room()
+    step(want)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step(other)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(other, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(rec)
+    for k in range(3):
+        if k:
+            x.copy_(x * 0.5 + 0.25)
+        if k == 2 and dtype == torch.float32:
+            x[:, 0] *= 1e9  # (fp32: the range of the rows decides in the kernels, not when they are recorded)
+            w[:, 0] *= 1e-9
+        step(want)
+        for r in rec:
+            r.fill_(3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(rec, want)), k
