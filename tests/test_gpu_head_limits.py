@@ -6,7 +6,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_head import ROUND, U, _close, _definition, _gen, _problem, ctx  # noqa: F401
+from test_gpu_head import ROUND, U, _definition, _gen, _problem, ctx  # noqa: F401
+from test_head_pieces import coherent
 
 pytestmark = pytest.mark.gpu
 
@@ -154,14 +155,9 @@ def test_one_uneven_row_among_blocks_of_rows(ctx, n, dim, vocab, at):  # noqa: F
 @pytest.mark.parametrize("kind", ["even", "one column"])
 @pytest.mark.parametrize("n,dim,vocab", [(16, 72, 2), (60, 64, 2), (200, 128, 2), (100, 192, 2), (2500, 264, 520), (70_000, 136, 24)])
 def test_no_piece_of_fp32_values_is_lost(ctx, n, dim, vocab, kind):  # noqa: F811
-    """Positive values whose second and third pieces all have one sign, so that a product of pieces that is left out or taken twice adds up: 2^-9 of a score or
-    2^-17 of it.  Two classes have weights and the rest a tenth of them, so the log of the normaliser shows the scores, and the gradients' sums have few large terms.
-    Bounds: 6 u of the sum of magnitudes for a score (roundings of dim / 32 partial sums and of the pieces, at random), 16 u where pieces are of fp16,
-    twice that for a gradient that has the score's error and its own."""
-    g = _gen(dim)
-    tail = 1.0 + 0.2 * 2.0 ** -8 + 0.2 * 2.0 ** -16  # (to the nearest 8 bits: 1, rest 0.2 * 2^-8 and so on)
-    grid = lambda *s: 0.25 * (1.0 + torch.randint(0, 128, s, generator=g) / 128.0) * (1.0 + 0.0 * torch.rand(s, generator=g))  # noqa: E731
-    x, w = (grid(n, dim).double() * tail).float(), (grid(vocab, dim).double() * tail).float()
+    """Values whose products of pieces add up, so that one that is left out, or taken twice, shows (test_head_pieces.py has what each would do).  Two classes have positive scores,
+    and the gradients' sums few large terms.  Bounds: 16 u of the sum of magnitudes for a score, for a gradient what that makes of p and 8 u of its own."""
+    x, w = coherent(n, dim, 1), coherent(vocab, dim, 2)
     w[2:] = -w[2:]
     if kind == "one column":
         x[:, 5] *= 2.0 ** 26
