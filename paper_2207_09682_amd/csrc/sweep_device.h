@@ -146,7 +146,7 @@ __device__ __forceinline__ void sweep(const SweepArgs& a) {
         const int q = j * 512 + tid, row = (q / CB) % TILE, c = (q % CB) ^ swept_turn<CB>(row);
         const int64_t ld = SP::F16 && MODE != SWEEP_STATS && q / (TILE * CB) < SP::SCORE ? a.dp : a.swept_ld;
         off[j] = (uint32_t)row * (uint32_t)(ld * 2) + (uint32_t)c * 16u;
-        at_row[j] = c * 8 < a.dp ? row : 1 << 30;
+        at_row[j] = c * 8 < a.dp ? row : 0x7fffffff;  // (never below the rows that are left)
     }
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)product_tiles;
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
