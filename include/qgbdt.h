@@ -320,8 +320,8 @@ QGBDT_API int qgbdt_boost_iteration_lambdarank(qgbdt_ctx* ctx, const void* bins,
  * None of these calls uses the context's shape or workspace; they work on a context with no workspace set.  Those that need
  * device scratch are handed it: `scratch` (dev, 256-byte aligned) of at least the bytes that the matching *_bytes
  * call says (QGBDT_E_WORKSPACE if smaller); its contents do not matter and mean nothing afterwards.  dtype is QGBDT_F32,
- * _BF16 or _F16 of all matrices of a call; sums and exponentials are fp32 or wider, results are rounded once to their type.
- * tokens and targets are int32 (token_bytes = 4) or int64 (8).  Matrices are row-major; strides count elements.  Calls
+ * _BF16 or _F16 of all matrices of a call; sums and exponentials are fp32 or wider, results are rounded once to their type (and
+ * D of qgbdt_softmax_gradients of _BF16, 2^-8 of each value, from 9 rows on, 17 where they have at most 256 values).  tokens and targets are int32 (token_bytes = 4) or int64 (8).  Matrices are row-major; strides count elements.  Calls
  * give the same bits every time. */
 
 /* out[i][:] = scale * sum over b of table[tokens[i][b]][:], b = 0 .. bag-1 (bag = 1: a plain lookup).  Tokens outside

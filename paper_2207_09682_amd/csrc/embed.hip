@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const typename E::T* __restr
 
 // ---- the gradient -----------------------------------------------------------------------------------
 // The entries (i, b) are sorted by token, ties by position, so that every sum has a fixed order.  A stable radix sort, least digit
-// first, of one or two digits of up to 10 bits (three beyond 2^20 tokens): a count per workgroup's tile and digit, sums over the tiles, and
+// first, of one or two digits of up to 10 bits (three beyond 2^20 tokens, four beyond 2^30): a count per workgroup's tile and digit, sums over the tiles, and
 // the move.  An entry is its token and its position; padding has the token n_vocab and comes last.
 
 constexpr int DIGIT_BITS = 10, DIGITS = 1 << DIGIT_BITS;
@@ -354,7 +354,7 @@ __device__ __forceinline__ void put_row(typename E::T* row, int c, int dim, cons
 //    go on while it waits for its tokens.
 //  * Tokens of up to unit entries: added up by the group that has the first one, `each` consecutive entries per group.
 // Bound by the zeros where the table is large (131,072 x 2048 bf16: 110 us of stores, 4.9 TB/s) and by requests to the caches where rows are short
-// (2.6 M rows of 256 bytes: 168 us, 4 TB/s).
+// (2.6 M rows of 256 bytes: 161 us, 4.2 TB/s: a group waits for an entry, its token's range, the token's entries and then two rows).
 template <class E, bool TINY>
 __global__ __launch_bounds__(256) void embed_sums_kernel(const typename E::T* __restrict__ grad, const uint2* __restrict__ entry, const int2* __restrict__ range,
                                                          int64_t m, int64_t n_vocab, int bag, int dim, int lanes, int unit, int unit_blocks, int each,
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(const typename E::T* __
 
 // Tokens of more than unit entries: such a token's entries go beyond the unit in which they begin, so a unit begins at most one.  A
 // workgroup looks at `each` units; its groups of lanes take the parts in turn and are added up in their order.
-constexpr int MERGE_THREADS = 256;  // (2.6 M entries, the most frequent token's 3750 parts: 26 us; with 1024: 109)
+constexpr int MERGE_THREADS = 256;  // (2.6 M entries, the most frequent token's 3750 parts: 30 us; with 1024: 109)
 template <class E, bool TINY>
 __global__ __launch_bounds__(MERGE_THREADS) void embed_merge_kernel(const uint2* __restrict__ entry, const int2* __restrict__ range, int64_t m, int64_t n_vocab, int unit, int64_t units, int each, int dim,
                                                           int lanes, const float* __restrict__ part, float scale, typename E::T* __restrict__ out, int accumulate) {

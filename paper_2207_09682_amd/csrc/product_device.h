@@ -152,12 +152,6 @@ struct FragReader {
 
 __host__ __device__ constexpr int product_lds(int bl, int br, int stages) { return stages * (bl + br) * PK * 2; }  // bytes
 
-// WL x WR wavefronts, each with (BL / WL) x (BR / WR) values of C.  A step is 64 values of k, two halves of 32, and STAGES steps are in
-// LDS or on their way.  Early in the second half of step t, whose operands are in registers by then, the wavefronts meet: everybody
-// has step t + 1 and has left the place of step t, which t + STAGES takes.  So operands of t + 1 are read during that half, and
-// the loads have STAGES - 1 steps to arrive.  Operands of r are read again into the registers of those just used.
-// A lane has C[l][r] of l = lane % 16 and r = 4 (lane / 16) + 0..3 of each block of 16 x 16: what is summed or stored along r lies in
-// few lanes.
 struct ProductPlace {
     int tl, tr, split;  // tile of l and of r, part of k
 };
@@ -176,6 +170,12 @@ __device__ __forceinline__ bool product_place(const ProductArgs& a, int block, P
     return true;
 }
 
+// WL x WR wavefronts, each with (BL / WL) x (BR / WR) values of C.  A step is 64 values of k, two halves of 32, and STAGES steps are in
+// LDS or on their way.  Early in the second half of step t, whose operands are in registers by then, the wavefronts meet: everybody
+// has step t + 1 and has left the place of step t, which t + STAGES takes.  So operands of t + 1 are read during that half, and
+// the loads have STAGES - 1 steps to arrive.  Operands of r are read again into the registers of those just used.
+// A lane has C[l][r] of l = lane % 16 and r = 4 (lane / 16) + 0..3 of each block of 16 x 16: what is summed or stored along r lies in
+// few lanes.
 template <int BL, int BR, int WL, int WR, int STAGES, bool F16, bool LT, bool RT>
 __device__ __forceinline__ void product_sums(const ProductArgs& a, const ProductPlace& at, f32x4 (&acc)[BL / WL / 16][BR / WR / 16]) {
     constexpr int T = 64 * WL * WR, NL = BL / WL / 16, NR = BR / WR / 16, STAGE = (BL + BR) * PK;

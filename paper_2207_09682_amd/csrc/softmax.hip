@@ -67,7 +67,7 @@ __device__ __forceinline__ float common_weight(const LeftOut& src, int64_t rows)
     return top ? __uint_as_float(top) : 1.0f;
 }
 
-// Up to WEIGHT_BLOCKS maxima of the rows' weights.  Bound by latency, with very many rows by memory (100,003 rows: 3 us).
+// Up to WEIGHT_BLOCKS maxima of the rows' weights.  Bound by latency, with very many rows by memory (100,003 rows: 5 us).
 __global__ __launch_bounds__(256) void weight_kernel(LeftOut src, int64_t rows, uint32_t* __restrict__ tops, uint32_t* __restrict__ range) {
     uint32_t top = 0;
     if (range && blockIdx.x == 0 && threadIdx.x == 0) *range = 0;  // (for lay_out_fp32_kernel)
@@ -133,7 +133,8 @@ struct Fp32Rows {
 
 // fp32 rows in two fp16 pieces for the scores, each row brought to 2^14 .. 2^15 by a power of two, which `back` undoes, and with THREE in
 // three bfloat16 pieces too, for the second products.  `lanes` threads have a row.  The first w_blocks workgroups lay out the weights, the others x.  What
-// the rows say about their pieces (RANGE_...) goes to a byte per workgroup or into *range.  Bound by memory (100,003 x 64 with all pieces: 14 us, 6 TB/s).
+// the rows say about their pieces (RANGE_...) goes to a byte per workgroup or into *range.  Bound by memory (100,003 x 64
+// and 10,007 classes with all pieces: 22 us, 4.5 TB/s; without the bfloat16 ones 16).
 template <bool THREE>
 __global__ __launch_bounds__(256) void lay_out_fp32_kernel(Fp32Rows w, Fp32Rows x, int w_blocks, int dim, int dp, int lanes, LeftOut of_x, uint8_t* __restrict__ marks,
                                                            uint32_t* __restrict__ range) {
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(256) void lay_out_fp32_kernel(Fp32Rows w, Fp32Rows 
 }
 
 // Between the layout and the scores of a loss: the range of all rows, and where it asks for them three bfloat16 pieces in place of the two of fp16.  before:
-// of the rows before these, whose pieces of the weights stay.
+// of the rows before these, whose pieces of the weights stay.  Bound by latency (5 us), by memory where pieces are made.
 __global__ __launch_bounds__(256) void settle_kernel(Fp32Rows w, Fp32Rows x, int dim, int dp, const uint8_t* __restrict__ marks, int n_marks, const uint32_t* __restrict__ before,
                                                      uint32_t* __restrict__ range) {
     __shared__ uint32_t found;
@@ -322,7 +323,8 @@ struct StatsEpilogue {
     }
 };
 
-// D of a strip of classes, in units of the common weight; rows and columns beyond the last ones, as far as the products read
+// D of a strip of classes, in units of the common weight.  PIECES = 1 rounds it to bfloat16, 2^-8 of each value, as the operand of the two products that
+// follow: two pieces would double these, two of the three products of a step, for gradients that are rounded to the same type.  PIECES = 3 keeps 24 bits.  Rows and columns beyond the last ones, as far as the products read
 // them, are zeros.  A lane has 4 consecutive values of a row: they are turned in LDS, so that 16 bytes per lane
 // and whole rows of the wavefront's part go to memory (8192 rows x 16,384 classes x 2048: 473 us; D^T X, a product of the same size, 412).
 template <int PIECES>
